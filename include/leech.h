@@ -482,6 +482,142 @@ int leech_transcode_planes14(const leech_layout_desc* desc, const void* d_index_
                              const uint64_t* d_code, void* d_main, uint32_t* d_bad,
                              void* stream);
 
+/* ------------------------- between a layer's q/k/v and o: cache and attention
+ * What a decoder layer does between its q/k/v product and its o product:
+ * rotary positions, a paged key/value cache, and the attention of new tokens
+ * over it.  Arrays of rows [T tokens][heads][dim] are given with their strides
+ * (in elements, any sign, unit stride along a head), so the columns of a fused
+ * product serve as they are. */
+enum { LEECH_F32 = 0, LEECH_F16 = 1, LEECH_BF16 = 2, LEECH_INT8 = 3, LEECH_E4M3 = 4 };
+
+typedef struct {
+  void* data;              /* device, aligned to an element; rows whose pointer and  */
+                           /* strides are multiples of 4 elements move 4 at a time   */
+  int32_t type;            /* LEECH_F32, LEECH_F16 or LEECH_BF16                     */
+  int64_t token_stride, head_stride;
+} leech_rows;
+
+/* Rotary positions.  A token at position p turns pair i of a head, i <
+ * width / 2, by the angle p · freq[i]:
+ *     a' = magnitude · (a cos − b sin),  b' = magnitude · (a sin + b cos),
+ * (a, b) the coordinates (i, i + width / 2), or (2i, 2i + 1) when interleaved;
+ * coordinates from width on stay as they are (no magnitude).  The angle is
+ * formed and reduced in f64, sine, cosine and the rotation are f32, the result
+ * is rounded once.  Schemes that stretch a model's range (positions divided by
+ * a factor, another base, either by frequency) are frequencies and a magnitude
+ * that the caller computes. */
+typedef struct {
+  const double* freq;      /* device, f64 [width / 2], radians a position, 8-byte    */
+                           /* aligned                                                */
+  float magnitude;         /* positive, finite                                       */
+  int32_t width;           /* a multiple of 8, at most the head's dimension          */
+  int32_t interleaved;     /* 0 or 1                                                 */
+} leech_rotary;
+
+/* out = x turned by its tokens' positions (int64 [T], device, any sign; an angle
+ * is off by at most 2^-51 of itself up to position 2^53).  transpose = 1 turns by the opposite angles, times the same
+ * magnitude: the gradient's pass, and the inverse where the magnitude is 1.  dim is a
+ * multiple of 8 up to 256; out's rows must not overlap one another; out may be
+ * x itself (same pointer, type and strides).  T = 0 does nothing.  Asynchronous on `stream`.
+ * LEECH_E_ARG for a NULL or misaligned pointer, an unknown type, a magnitude
+ * that is not positive and finite; LEECH_E_SHAPE for sizes outside the ranges
+ * above or output rows that overlap. */
+int leech_rope(int64_t T, int32_t heads, int32_t dim, const leech_rows* x,
+               const int64_t* d_positions, const leech_rotary* rotary, int transpose,
+               const leech_rows* out, void* stream);
+
+/* A paged key/value cache in caller-owned device memory.  A slot is page ·
+ * page_size + place; its head h is kept at
+ *     keys    k[((page · heads + h) · page_size + place) · dim + d]
+ *     values  v[((page · heads + h) · page_size + (place − place % I)) · dim
+ *               + d · I + place % I],   I = 16 / bytes of an element:
+ * sixteen bytes hold I consecutive places' values of one coordinate, as the
+ * attention's matrix products take them.  16-bit caches hold the rounded
+ * numbers.  8-bit caches hold codes, and an f32 scale per (page, head, place)
+ * for keys and for values: scale = largest magnitude of the row / 127 (int8)
+ * or / 448 (e4m3), code = x / scale to the nearest (ties to even), 0 in a row
+ * whose scale is 0; a row with a number that is not finite gets the scale NaN
+ * and reads as NaN. */
+typedef struct {
+  int32_t type;            /* LEECH_F16, LEECH_BF16, LEECH_INT8 or LEECH_E4M3        */
+  int32_t heads, dim;      /* dim a multiple of 16 up to 256                         */
+  int32_t page_size;       /* a power of two, 16 to 65536                            */
+  int64_t pages;
+  void *k, *v;             /* 16-byte aligned, pages · heads · page_size · dim each  */
+  float *k_scale, *v_scale; /* [pages][heads][page_size]; 8-bit caches only          */
+} leech_kv_cache;
+
+/* Write T tokens' keys and values into their slots (int64 [T], device), the
+ * keys turned first where a rotary is given (NULL: as they are; d_positions as
+ * leech_rope, else unused).  A slot below 0 or past the cache is skipped (a
+ * padded batch's rows); slots must differ, or which token's numbers a shared
+ * slot holds is open.  q_heads > 0 (with a rotary) also turns q into q_out in
+ * the same launch, for every token; q_out may be q itself.  Asynchronous on `stream`.
+ * LEECH_E_ARG and LEECH_E_SHAPE as leech_rope, and for a cache that is not as
+ * described. */
+int leech_cache_write(const leech_kv_cache* cache, int64_t T, const leech_rows* k,
+                      const leech_rows* v, const int64_t* d_slots, const int64_t* d_positions,
+                      const leech_rotary* rotary, int32_t q_heads, const leech_rows* q,
+                      const leech_rows* q_out, void* stream);
+
+/* Read T slots back as rows of f32, f16 or bf16 (code · scale, rounded once);
+ * a slot below 0 or past the cache reads as zeros.  Slots may repeat.
+ * Asynchronous on `stream`. */
+int leech_cache_read(const leech_kv_cache* cache, int64_t T, const int64_t* d_slots,
+                     const leech_rows* k_out, const leech_rows* v_out, void* stream);
+
+/* Attention of each sequence's new tokens over its cached ones.  Sequence b
+ * has n_b = q_start[b + 1] − q_start[b] new tokens, rows q_start[b].. of q, and
+ * L_b = kv_len[b] cached tokens, the new ones among them (written before this
+ * call): token j in place j % page_size of page page_table[b][j / page_size].
+ * Its query i is at position p = L_b − n_b + i and sees the tokens j < L_b with
+ * j ≤ p (causal = 1) and j > p − window (window > 0).  With s_j = scale · q·k_j
+ * over the tokens seen, out = Σ e^(s_j − m) v_j / Σ e^(s_j − m), lse = m +
+ * ln Σ e^(s_j − m), m their largest; a query that sees nothing gets zeros and
+ * −inf.  Query head h reads cache head h / (q_heads / heads).
+ *
+ * Products are on the matrix cores, in q's type (8-bit codes are exact in
+ * either), sums, maxima and scales in f32; the weights e^(s_j − m) are rounded to
+ * q's type for the second product.  Rows of q and out before q_start[0] or from
+ * q_start[B] on are not read or written.  Lengths, starts and pages are read on
+ * the device; what lies out of range there stays in bounds: starts are clamped
+ * to [0, T], L_b to [0, table_pages · page_size], and a page that is not in
+ * [0, pages) makes the rows that see it NaN.  A number that is not finite, in a
+ * key, value or scale, reaches only the rows that see its token, and makes
+ * them not finite; what pages hold from L_b on never matters.  The result does
+ * not depend on the other sequences' contents, but on how the work is split,
+ * which goes by all lengths. */
+typedef struct {
+  int32_t type;            /* of q and out: LEECH_F16 or LEECH_BF16; a 16-bit cache  */
+                           /* must have the same                                     */
+  int32_t q_heads;         /* a multiple of the cache's heads                        */
+  int64_t T;               /* rows of q and out                                      */
+  const void* q;           /* 16-byte aligned, strides multiples of 8 elements       */
+  int64_t q_token_stride, q_head_stride;
+  void* out;               /* as q; its rows must not overlap                        */
+  int64_t out_token_stride, out_head_stride;
+  float* lse;              /* [T][q_heads], or NULL                                  */
+  int32_t B;               /* sequences                                              */
+  const int32_t* q_start;  /* [B + 1], ascending; NULL: one new token a sequence     */
+                           /* (T = B)                                                */
+  const int32_t* kv_len;   /* [B]                                                    */
+  const int32_t* page_table;  /* [B] rows of table_pages, table_stride apart         */
+  int64_t table_stride;
+  int32_t table_pages;
+  int32_t max_new;         /* at least every n_b (rows past it are left as they are) */
+  int32_t causal;          /* 0 or 1                                                 */
+  int32_t window;          /* 0: none                                                */
+  float scale;             /* finite                                                 */
+  void* workspace;         /* leech_attend_workspace bytes, 16-byte aligned, this    */
+  size_t workspace_bytes;  /* call's own until it is done; NULL where that is 0      */
+} leech_attend_args;
+
+/* Bytes of workspace that leech_attend needs for these arguments (pointers and
+ * strides are not looked at; a function of the sizes alone). */
+int leech_attend_workspace(const leech_kv_cache* cache, const leech_attend_args* args,
+                           size_t* bytes);
+int leech_attend(const leech_kv_cache* cache, const leech_attend_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,13 +19,15 @@ from ._lib import (GOLAY70, LAYOUT_NAMES, LAYOUTS, PLANES12X, PLANES14, SLOT32, 
                    set_exception_mode,
                    EXC_HOISTED, EXC_INLINE, set_prologue_mode, PROLOGUE_AUTO,
                    set_batch_mode, BATCH_AUTO, BATCH_DOT2)
+from .kv import KVCache, Rotary, rope, rotary_frequencies
 
 __all__ = ["Codebook", "DeviceCodebook", "LeechMatrix", "LayoutDesc", "LeechError", "LAYOUTS",
            "LAYOUT_NAMES", "SLOT32", "PLANES14", "PLANES12X", "GOLAY70", "expand_layout",
            "host_decode_layout", "layout_scales", "fp16_gemv", "noweights_ctrl", "rotate_x",
            "index_encode", "index_decode", "planes14_desc", "layout_geometry", "set_exception_mode",
            "EXC_HOISTED", "EXC_INLINE", "set_prologue_mode", "PROLOGUE_AUTO",
-           "set_batch_mode", "BATCH_AUTO", "BATCH_DOT2"]
+           "set_batch_mode", "BATCH_AUTO", "BATCH_DOT2", "KVCache", "Rotary", "rope",
+           "rotary_frequencies"]
 
 
 def _torch():

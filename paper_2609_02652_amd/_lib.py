@@ -31,7 +31,10 @@ EXPORTS = ["leech_last_error", "leech_codebook_build", "leech_codebook_free",
            "leech_index_encode", "leech_index_decode", "leech_planes14_desc",
            "leech_transcode_planes14", "leech_set_exception_mode", "leech_gemv_batch",
            "leech_gemv_rotated", "leech_set_prologue_mode", "leech_set_batch_mode",
-           "leech_expand_layout_tiled", "leech_layout_geometry", "leech_gemv_phases"]
+           "leech_expand_layout_tiled", "leech_layout_geometry", "leech_gemv_phases",
+           "leech_rope", "leech_cache_write", "leech_cache_read", "leech_attend_workspace",
+           "leech_attend"]
+F32, F16, BF16, INT8, E4M3 = 0, 1, 2, 3, 4
 
 
 class LeechError(RuntimeError):
@@ -53,6 +56,33 @@ class LayoutDesc(C.Structure):
                 "main_bytes": self.main_bytes,
                 "side_bytes": [self.side_bytes[0], self.side_bytes[1]],
                 "n_exceptions": self.n_exceptions, "served_bytes": self.served_bytes}
+
+
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("type", C.c_int32), ("token_stride", C.c_int64),
+                ("head_stride", C.c_int64)]
+
+
+class RotaryDesc(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("magnitude", C.c_float), ("width", C.c_int32),
+                ("interleaved", C.c_int32)]
+
+
+class KVCacheDesc(C.Structure):
+    _fields_ = [("type", C.c_int32), ("heads", C.c_int32), ("dim", C.c_int32),
+                ("page_size", C.c_int32), ("pages", C.c_int64), ("k", C.c_void_p),
+                ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class AttendArgs(C.Structure):
+    _fields_ = [("type", C.c_int32), ("q_heads", C.c_int32), ("T", C.c_int64),
+                ("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("out", C.c_void_p), ("out_token_stride", C.c_int64),
+                ("out_head_stride", C.c_int64), ("lse", C.c_void_p), ("B", C.c_int32),
+                ("q_start", C.c_void_p), ("kv_len", C.c_void_p), ("page_table", C.c_void_p),
+                ("table_stride", C.c_int64), ("table_pages", C.c_int32), ("max_new", C.c_int32),
+                ("causal", C.c_int32), ("window", C.c_int32), ("scale", C.c_float),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
 def _load() -> C.CDLL:
@@ -103,6 +133,16 @@ def _load() -> C.CDLL:
                                  P]),
         "leech_gemv_rotated": (I, [C.POINTER(LayoutDesc), P, P, P, P, P, P, I, P, P, I64, P, P,
                                    P, P]),
+        "leech_rope": (I, [I64, I32, I32, C.POINTER(Rows), P, C.POINTER(RotaryDesc), I,
+                           C.POINTER(Rows), P]),
+        "leech_cache_write": (I, [C.POINTER(KVCacheDesc), I64, C.POINTER(Rows), C.POINTER(Rows),
+                                  P, P, C.POINTER(RotaryDesc), I32, C.POINTER(Rows),
+                                  C.POINTER(Rows), P]),
+        "leech_cache_read": (I, [C.POINTER(KVCacheDesc), I64, P, C.POINTER(Rows),
+                                 C.POINTER(Rows), P]),
+        "leech_attend_workspace": (I, [C.POINTER(KVCacheDesc), C.POINTER(AttendArgs),
+                                       C.POINTER(C.c_size_t)]),
+        "leech_attend": (I, [C.POINTER(KVCacheDesc), C.POINTER(AttendArgs), P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -370,3 +410,34 @@ def set_prologue_mode(mode: int) -> None:
     """Process-wide: the order in which single GEMVs enqueued afterwards request
     their records (PROLOGUE_AUTO, or 0, 1, 2); y does not depend on it."""
     check(lib.leech_set_prologue_mode(mode))
+
+
+# Rows, RotaryDesc, KVCacheDesc and AttendArgs are passed by reference; None is
+# NULL (an absent rotary, no queries).
+def rope(T, heads, dim, x, d_positions, rotary, transpose, out, stream=0):
+    check(lib.leech_rope(T, heads, dim, x, d_positions, rotary, int(transpose), out,
+                         stream or None))
+
+
+def check_cache(cache) -> None:
+    """Refuses a cache that the library would: a read of no token."""
+    check(lib.leech_cache_read(cache, 0, None, None, None, None))
+
+
+def cache_write(cache, T, k, v, d_slots, d_positions, rotary, q_heads, q, q_out, stream=0):
+    check(lib.leech_cache_write(cache, T, k, v, d_slots, d_positions, rotary, q_heads, q, q_out,
+                                stream or None))
+
+
+def cache_read(cache, T, d_slots, k_out, v_out, stream=0):
+    check(lib.leech_cache_read(cache, T, d_slots, k_out, v_out, stream or None))
+
+
+def attend_workspace(cache, args) -> int:
+    n = C.c_size_t()
+    check(lib.leech_attend_workspace(cache, args, n))
+    return n.value
+
+
+def attend(cache, args, stream=0):
+    check(lib.leech_attend(cache, args, stream or None))
