@@ -544,7 +544,8 @@ typedef struct {
   int32_t page_size;       /* a power of two, 16 to 65536                            */
   int64_t pages;
   void *k, *v;             /* 16-byte aligned, pages · heads · page_size · dim each  */
-  float *k_scale, *v_scale; /* [pages][heads][page_size]; 8-bit caches only          */
+  float *k_scale, *v_scale; /* [pages][heads][page_size], 16-byte aligned; 8-bit     */
+                           /* caches only                                            */
 } leech_kv_cache;
 
 /* Write T tokens' keys and values into their slots (int64 [T], device), the
@@ -576,9 +577,10 @@ int leech_cache_read(const leech_kv_cache* cache, int64_t T, const int64_t* d_sl
  * ln Σ e^(s_j − m), m their largest; a query that sees nothing gets zeros and
  * −inf.  Query head h reads cache head h / (q_heads / heads).
  *
- * Products are on the matrix cores, in q's type (8-bit codes are exact in
- * either), sums, maxima and scales in f32; the weights e^(s_j − m) are rounded to
- * q's type for the second product.  Rows of q and out before q_start[0] or from
+ * Products are on the matrix cores with f32 sums, in the type of a 16-bit cache;
+ * over an 8-bit one in f16, which holds every code (bf16 queries enter it times
+ * a power of two a row).  Maxima, sums and scales are f32; the weights
+ * e^(s_j − m) are rounded to the products' type for the second one.  Rows of q and out before q_start[0] or from
  * q_start[B] on are not read or written.  Lengths, starts and pages are read on
  * the device; what lies out of range there stays in bounds: starts are clamped
  * to [0, T], L_b to [0, table_pages · page_size], and a page that is not in

@@ -1,14 +1,39 @@
 // Attention of new tokens over the paged key/value cache for gfx950.
 //
-// A wave owns one query row (a token's query head) and walks the keys it sees
-// in blocks of 64, a lane a key: scores, their running maximum and sum (one
-// pass: what is summed so far is scaled down when the maximum grows), then the
-// weighted values, a lane a coordinate.
+// Both products run transposed on the matrix cores: Sᵀ = K Qᵀ, then Oᵀ = Vᵀ Pᵀ,
+// in 16×16×32 products.  A lane then holds, for one query (its column), the
+// scores of the tokens whose values it feeds to the second product, so weights
+// go from one product to the next in the lane's own registers; the maximum and
+// the sum of a query are two exchanges across the wave's four quarters; and the
+// rescaling of Oᵀ is by one factor a lane.  Keys are rows as they lie (sixteen
+// bytes a lane); row m of the u-th key tile is token I·(m / 4) + 4u + m % 4 of
+// the step, so that quarter g of the wave ends up with the scores of tokens
+// I·g .. I·g + I − 1, the run of tokens that sixteen bytes of the value pages
+// hold.  Both operands come from memory straight into the registers that the
+// products read.
+//
+// One pass: the running maximum m and sum l of e^(s − m); when m grows, l and O
+// are scaled down.  Rows are (new token, query head of the group) of one
+// sequence and cache head, so a group's heads share every key read.
+//
+// 8-bit codes become f16, which holds all of them; a key's scale multiplies its
+// scores, a value's scale its weight, over the query's largest such scale so
+// far (weights under f16's range would lose bits).  bf16 queries over 8-bit
+// codes become f16 times a power of two a row.
 
 #include "kv_device.h"
 
+#include <algorithm>
+
 namespace leech {
 namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLn2 = 0.69314718055994531f;
 
 struct AttendArgs {
   CacheShape c;
@@ -21,7 +46,23 @@ struct AttendArgs {
   const int32_t *q_start, *kv_len, *table;
   int64_t T, pages;
   int32_t type, q_heads, group, B, table_pages, max_new, causal, window;
-  float scale;
+  float scale;                // times log2 e
+  // how the work is cut (see Plan)
+  int32_t block_rows, log_step, min_steps, units, split;
+  float target;
+  float *part_o, *part_ml;    // [head][unit][row][dim], [head][unit][row][2]
+};
+
+// ------------------------------------------------------------------- the plan
+// A sequence's rows are cut in tiles of block_rows, its keys in steps of
+// 2^log_step tokens, and the steps that a sequence's rows see in equal parts, so
+// many that all parts of all sequences together come to about `target`
+// workgroups of equal work (never less than min_steps a part).  A unit is a part
+// of a tile; units are numbered sequence by sequence, tile by tile.  Every wave
+// works the numbering out for itself, a lane a sequence.
+struct Sequence {
+  int64_t first;              // row of q of its first new token
+  int32_t n, rows, tiles, len, steps, parts;
 };
 
 __device__ __forceinline__ int64_t start_of(const AttendArgs& a, int b) {
@@ -29,99 +70,615 @@ __device__ __forceinline__ int64_t start_of(const AttendArgs& a, int b) {
   return s < 0 ? 0 : s > a.T ? a.T : s;
 }
 
-__device__ __forceinline__ float element(const uint8_t* p, int type, int64_t at) {
-  if (type == LEECH_INT8) return (float)((const int8_t*)p)[at];
-  if (type == LEECH_E4M3) return __builtin_amdgcn_cvt_f32_fp8((int)p[at], 0);
-  const uint32_t h = ((const uint16_t*)p)[at];
-  return type == LEECH_F16 ? half_value(h) : bf16_value(h);
+__device__ __forceinline__ Sequence sequence(const AttendArgs& a, int b) {
+  Sequence s = {0, 0, 0, 0, 0, 0, 1};
+  if (b >= a.B) return s;
+  s.first = start_of(a, b);
+  const int64_t n = start_of(a, b + 1) - s.first;
+  s.n = n < 0 ? 0 : (int32_t)n;
+  s.rows = (s.n < a.max_new ? s.n : a.max_new) * a.group;
+  s.tiles = (s.rows + a.block_rows - 1) / a.block_rows;
+  const int64_t room = (int64_t)a.table_pages << a.c.log_page;
+  const int32_t len = a.kv_len[b];
+  s.len = len < 0 ? 0 : len > room ? (int32_t)room : len;
+  int64_t lo = a.window ? (int64_t)s.len - s.n - a.window + 1 : 0;
+  if (lo < 0) lo = 0;
+  s.steps = ((s.len + (1 << a.log_step) - 1) >> a.log_step) - (int32_t)(lo >> a.log_step);
+  if (s.steps < 1) s.steps = 1;
+  return s;
 }
 
-__global__ __launch_bounds__(64) void attend_kernel(AttendArgs a) {
-  __shared__ float qs[kMaxHeadDim];
-  __shared__ float ws[64];
-  __shared__ int64_t where[64];
-  const int lane = threadIdx.x, h = blockIdx.y, d0 = a.c.dim;
-  const int64_t t = blockIdx.x;
-  int lo = 0, hi = a.B;                     // the last sequence that starts at or before t
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (start_of(a, mid + 1) <= t)
-      lo = mid + 1;
-    else
-      hi = mid;
+__device__ __forceinline__ int wave_scan(int v) {       // inclusive
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(v, d, 64);
+    if (lane >= d) v += o;
   }
-  if (lo >= a.B || start_of(a, lo) > t) return;
-  const int64_t first = start_of(a, lo), n = start_of(a, lo + 1) - first, i = t - first;
-  if (i >= a.max_new) return;
-  int64_t len = a.kv_len[lo];
-  const int64_t room = (int64_t)a.table_pages << a.c.log_page;
-  len = len < 0 ? 0 : len > room ? room : len;
-  const int64_t p = len - n + i;
-  const int64_t to = a.causal && p + 1 < len ? p + 1 : len;
-  int64_t from = a.window ? p - a.window + 1 : 0;
-  if (from < 0) from = 0;
-  const int type = a.c.type;
-  for (int d = lane; d < d0; d += 64) {
-    const uint32_t x = a.q[t * a.q_token + h * a.q_head + d];
-    qs[d] = a.type == LEECH_F16 ? half_value(x) : bf16_value(x);
+  return v;
+}
+
+// The sequence, and the number of its first unit, of unit `unit` (by_unit) or of
+// row `token` of q; false if there is none.
+__device__ __forceinline__ bool find(const AttendArgs& a, bool by_unit, int unit, int64_t token,
+                                     Sequence* out, int* seq, int* first_unit) {
+  const int lane = threadIdx.x & 63;
+  const Sequence head = sequence(a, lane);
+  int steps = 0x7fffffff;                               // of a part
+  if (a.split) {
+    float total = 0.0f;
+    for (int b = 0; b < a.B; b += 64) {
+      const Sequence s = b ? sequence(a, b + lane) : head;
+      float w = (float)s.tiles * (float)s.steps;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) w += __shfl_xor(w, d, 64);
+      total += w;
+    }
+    const float share = ceilf(total * (float)a.c.heads / a.target);
+    steps = share > 1e9f ? 1000000000 : share > (float)a.min_steps ? (int)share : a.min_steps;
   }
-  __syncthreads();
-  float m = -__builtin_inff(), l = 0.0f, o[4] = {0, 0, 0, 0};
-  const int kh = h / a.group;
-  for (int64_t j0 = from; j0 < to; j0 += 64) {
-    const int64_t j = j0 + lane;
-    float s = -__builtin_inff();
-    int64_t slot = -1;
-    if (j < to) {
-      const int64_t page = a.table[lo * a.table_stride + (j >> a.c.log_page)];
-      if (page < 0 || page >= a.pages) {
-        s = __builtin_nanf("");
-      } else {
-        slot = (page << a.c.log_page) + (j & ((1 << a.c.log_page) - 1));
-        const int64_t at = key_at(a.c, slot, kh);
-        s = 0.0f;
-        for (int d = 0; d < d0; ++d) s += qs[d] * element(a.ck, type, at + d);
-        s *= a.scale;
-        if (type_bytes(type) == 1) s *= a.sk[scale_at(a.c, slot, kh)];
+  int before = 0;
+  for (int b = 0; b < a.B; b += 64) {
+    Sequence s = b ? sequence(a, b + lane) : head;
+    s.parts = a.split ? (s.steps + steps - 1) / steps : 1;
+    const int own = s.tiles * s.parts, upto = before + wave_scan(own);
+    const bool hit = by_unit ? unit >= upto - own && unit < upto
+                             : token >= s.first && token - s.first < (s.n < a.max_new ? s.n : a.max_new);
+    const uint64_t mask = __ballot(hit);
+    if (mask) {
+      const int at = __ffsll((unsigned long long)mask) - 1;
+      out->first = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)s.first, at);
+      out->n = __builtin_amdgcn_readlane(s.n, at);
+      out->rows = __builtin_amdgcn_readlane(s.rows, at);
+      out->tiles = __builtin_amdgcn_readlane(s.tiles, at);
+      out->len = __builtin_amdgcn_readlane(s.len, at);
+      out->steps = __builtin_amdgcn_readlane(s.steps, at);
+      out->parts = __builtin_amdgcn_readlane(s.parts, at);
+      *seq = b + at;
+      *first_unit = __builtin_amdgcn_readlane(upto - own, at);
+      return true;
+    }
+    before = __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+// The keys [lo, hi) that row r of a sequence sees.
+__device__ __forceinline__ void row_range(const AttendArgs& a, const Sequence& s, int r, int& lo,
+                                          int& hi) {
+  const int64_t p = (int64_t)s.len - s.n + r / a.group;
+  hi = a.causal && p + 1 < s.len ? (p + 1 < 0 ? 0 : (int)(p + 1)) : s.len;
+  const int64_t l = a.window ? p - a.window + 1 : 0;
+  lo = l < 0 ? 0 : l > hi ? hi : (int)l;
+}
+
+// ------------------------------------------------------------------ the waves
+enum { kF16 = 0, kBf16 = 1, kInt8 = 2, kE4m3 = 3 };       // what the cache holds
+template <int CT>
+constexpr int kBytes = CT < 2 ? 2 : 1;
+template <int CT>
+constexpr int kRun = 16 / kBytes<CT>;                     // tokens a run
+template <int CT>
+constexpr int kStep = 4 * kRun<CT>;                       // tokens a wave takes at once
+
+template <int CT>
+__device__ __forceinline__ f32x4 mfma16(kv_u32x4 a, kv_u32x4 b, f32x4 c) {
+  if constexpr (CT == kBf16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Two f32 to a pair of the type that the products take, to nearest.
+template <int CT>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  if constexpr (CT == kBf16) {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, b2{(__bf16)a, (__bf16)b});
+  } else {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, h2{(_Float16)a, (_Float16)b});
+  }
+}
+
+// Four codes (a word) to two pairs of f16.
+template <int CT>
+__device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  if constexpr (CT == kInt8) {
+    // code + 128 as the low byte of a half of 1024 is 1152 + code
+    w ^= 0x80808080u;
+    const h2 off = {(_Float16)1152.0f, (_Float16)1152.0f};
+    lo = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u)) - off);
+    hi = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u)) - off);
+  } else {
+    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, false));
+    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, true));
+  }
+}
+// The h-th operand of eight elements that sixteen bytes hold.
+template <int CT>
+__device__ __forceinline__ kv_u32x4 operand(kv_u32x4 w, int h) {
+  if constexpr (kBytes<CT> == 2) return w;
+  uint32_t o[4];
+  widen<CT>(h ? w.z : w.x, o[0], o[1]);
+  widen<CT>(h ? w.w : w.y, o[2], o[3]);
+  return kv_u32x4{o[0], o[1], o[2], o[3]};
+}
+
+// v of the wave's quarters 0, 0, 2, 2 and 1, 1, 3, 3 (across: 32), or of its
+// halves (64).  The exchange swaps two registers in place: given one value
+// twice, the compiler names one register twice, so the copy is made opaque.
+struct Pair {
+  float a, b;
+};
+template <int ACROSS>
+__device__ __forceinline__ Pair swapped(float v) {
+  uint32_t x = __builtin_bit_cast(uint32_t, v), y = x;
+  asm("" : "+v"(y));
+  if constexpr (ACROSS == 32) {
+    const auto p = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+    return {__builtin_bit_cast(float, (uint32_t)p[0]), __builtin_bit_cast(float, (uint32_t)p[1])};
+  } else {
+    const auto p = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+    return {__builtin_bit_cast(float, (uint32_t)p[0]), __builtin_bit_cast(float, (uint32_t)p[1])};
+  }
+}
+// Largest, and sum, over the wave's four quarters (lanes l, l ^ 16, l ^ 32, l ^ 48).
+__device__ __forceinline__ float quarters_max(float v) {
+  Pair p = swapped<32>(v);
+  p = swapped<64>(fmaxf(p.a, p.b));
+  return fmaxf(p.a, p.b);
+}
+__device__ __forceinline__ float quarters_sum(float v) {
+  Pair p = swapped<32>(v);
+  p = swapped<64>(p.a + p.b);
+  return p.a + p.b;
+}
+
+// Bit e of the result: element e of the run w holds is not finite; those become 0.
+template <int CT>
+__device__ __forceinline__ uint32_t drop_non_finite(kv_u32x4& w) {
+  uint32_t bad = 0;
+  if constexpr (kBytes<CT> == 2) {
+    constexpr uint32_t ones = CT == kF16 ? 0x7C00u : 0x7F80u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t h = w[e >> 1] >> (16 * (e & 1));
+      if ((h & ones) == ones) {
+        bad |= 1u << e;
+        w[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
       }
     }
-    float top = s;
-    for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
-    const float mn = fmaxf(m, top);
-    const float base = mn == -__builtin_inff() ? 0.0f : mn;
-    const float w = j < to ? expf(s - base) : 0.0f, old = expf(m - base);
-    float sum = w;
-    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
-    l = l * old + sum;
-    m = mn;
-    __syncthreads();
-    ws[lane] = slot >= 0 && type_bytes(type) == 1 ? w * a.sv[scale_at(a.c, slot, kh)] : w;
-    where[lane] = slot;
-    __syncthreads();
-    for (int e = 0; e < 4; ++e) {
-      const int d = lane + 64 * e;
-      if (d >= d0) break;
-      float x = o[e] * old;
-      for (int k = 0; k < 64 && j0 + k < to; ++k)
-        x += where[k] < 0 ? ws[k]
-                          : ws[k] * element(a.cv, type,
-                                            value_at(a.c, where[k], kh) + d * value_run(type));
-      o[e] = x;
+  } else if constexpr (CT == kE4m3) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if ((w[e >> 2] >> (8 * (e & 3)) & 0x7Fu) == 0x7Fu) {
+        bad |= 1u << e;
+        w[e >> 2] &= ~(0xFFu << (8 * (e & 3)));
+      }
+  }
+  return bad;
+}
+
+constexpr int kWaves = 4;
+
+// A workgroup is a unit of up to 16·NT rows; its waves take the unit's steps in
+// turn and join at the end.  DT: the head's dimension, or the next of 64, 128,
+// 256 above it.  What bounds it is the cache's bytes: a step's keys and values
+// are 32 registers a lane each at DT = 128, the next step's keys loading while
+// this one's weights and values are worked on and the other way round.
+template <int CT, int DT, int NT>
+__global__ __launch_bounds__(64 * kWaves) void stream_kernel(AttendArgs a) {
+  constexpr int R = kRun<CT>, TOK = kStep<CT>, NU = R / 4;
+  constexpr int KC = DT * kBytes<CT> / 64;       // sixteen-byte loads of a key row's lane
+  constexpr int KM = DT / 32;                    // products along a head
+  constexpr int VM = DT / 16;                    // tiles of coordinates
+  constexpr int H = kBytes<CT> == 2 ? 1 : 2;     // operands in sixteen bytes
+  constexpr int COLS = 64;                       // coordinates joined at once
+  __shared__ float joined[kWaves][16 * NT][COLS + 4];
+  __shared__ float stats[kWaves][16 * NT][2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int h = blockIdx.x % a.c.heads, unit = blockIdx.x / a.c.heads;
+  Sequence s;
+  int b, u0;
+  if (!find(a, true, unit, 0, &s, &b, &u0)) return;
+  const int tile = (unit - u0) / s.parts, part = (unit - u0) % s.parts;
+  const int row0 = tile * a.block_rows;
+  const int rows = s.rows - row0 < 16 * NT ? s.rows - row0 : 16 * NT;
+  const int col = lane & 15, g = lane >> 4;
+
+  // the tile's keys, and those that every one of its rows sees
+  int lo_first, hi_first, lo_last, hi_last;
+  row_range(a, s, row0, lo_first, hi_first);
+  row_range(a, s, row0 + rows - 1, lo_last, hi_last);
+  int step0 = lo_first / TOK, step1 = (hi_last + TOK - 1) / TOK;
+  if (step1 < step0) step1 = step0;
+  const int64_t span = step1 - step0;
+  step1 = step0 + (int)(span * (part + 1) / s.parts);
+  step0 = step0 + (int)(span * part / s.parts);
+
+  int lo[NT], hi[NT];
+  kv_u32x4 qf[NT][KM];
+  float qs[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int r = row0 + 16 * t + col;
+    const bool in = 16 * t + col < rows;
+    lo[t] = hi[t] = 0;
+    if (in) row_range(a, s, r, lo[t], hi[t]);
+    const uint16_t* q = a.q + (s.first + r / a.group) * a.q_token +
+                        ((int64_t)h * a.group + r % a.group) * a.q_head;
+#pragma unroll
+    for (int m = 0; m < KM; ++m) {
+      // the coordinates that sixteen bytes of a key hold, in their order
+      const int d = H == 1 ? 32 * m + 8 * g : 64 * (m / 2) + 16 * g + 8 * (m % 2);
+      qf[t][m] = in && d < a.c.dim ? *(const kv_u32x4*)(q + d) : kv_u32x4{0, 0, 0, 0};
+    }
+    qs[t] = a.scale;
+    if (H == 2 && a.type == LEECH_BF16) {
+      // to f16, the row's largest just below 2^15: what falls under f16's range
+      // there is under 2^-39 of the largest
+      float big = 0.0f;
+#pragma unroll
+      for (int m = 0; m < KM; ++m)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          big = fmaxf(big, __builtin_fabsf(bf16_value(qf[t][m][e >> 1] >> (16 * (e & 1)) & 0xFFFFu)));
+      big = quarters_max(big);
+      int ex = (int)(__builtin_bit_cast(uint32_t, big) >> 23 & 0xFF) - 127 - 14;
+      ex = big > 0.0f && big < __builtin_inff() ? ex : 0;
+#pragma unroll
+      for (int m = 0; m < KM; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t w = qf[t][m][e];
+          qf[t][m][e] = pack2<kF16>(ldexpf(bf16_value(w & 0xFFFFu), -ex),
+                                    ldexpf(bf16_value(w >> 16), -ex));
+        }
+      qs[t] = ldexpf(a.scale, ex);
     }
   }
-  const float inv = l != 0.0f ? 1.0f / l : 0.0f;     // a NaN sum stays one
-  for (int e = 0; e < 4; ++e) {
-    const int d = lane + 64 * e;
-    if (d < d0)
-      a.out[t * a.o_token + h * a.o_head + d] =
-          (uint16_t)(a.type == LEECH_F16 ? half_bits(o[e] * inv) : bf16_bits(o[e] * inv));
+
+  f32x4 o[NT][VM];
+  float m[NT], l[NT], vref[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    m[t] = -__builtin_inff();
+    l[t] = vref[t] = 0.0f;
+#pragma unroll
+    for (int v = 0; v < VM; ++v) o[t][v] = f32x4{0, 0, 0, 0};
   }
-  if (a.lse && lane == 0) a.lse[t * a.q_heads + h] = l != 0.0f ? m + logf(l) : -__builtin_inff();
+
+  // A key lane reads run col / 4 of the step, a value lane run g.
+  const int row_bytes = a.c.dim * kBytes<CT>;
+  const int page_mask = (1 << a.c.log_page) - 1;
+  const int32_t* table = a.table + b * a.table_stride;
+  const int first_run = lo_first & ~(R - 1), last_run = (hi_last - 1) & ~(R - 1);
+  const auto run_at = [&](int step, int run) {
+    const int j = step * TOK + R * run;
+    return j < first_run ? first_run : j > last_run ? last_run : j;
+  };
+  const auto page_of = [&](int j) { return table[j >> a.c.log_page]; };
+  const auto place = [&](int page, int j) {          // slot, in units of slots of one head
+    const int p = page < 0 || page >= a.pages ? 0 : page;
+    return (((int64_t)p * a.c.heads + h) << a.c.log_page) + (j & page_mask);
+  };
+  kv_u32x4 kw[NU][KC], vw[VM];
+  float ks[R], vs[R];
+  const auto load_keys = [&](int page, int j) {
+    const uint8_t* row = a.ck + (place(page, j) + (col & 3)) * row_bytes;
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        const int at = 64 * c + 16 * g;
+        kw[u][c] = *(const kv_u32x4*)(row + 4 * u * row_bytes + (at < row_bytes ? at : 0));
+      }
+  };
+  const auto load_values = [&](int page, int j) {
+    const int64_t at = place(page, j);
+    const uint8_t* run = a.cv + at * row_bytes + 16 * col;
+#pragma unroll
+    for (int v = 0; v < VM; ++v)
+      if (16 * v < a.c.dim) vw[v] = *(const kv_u32x4*)(run + 256 * v);
+    if constexpr (H == 2) {
+#pragma unroll
+      for (int e = 0; e < R; e += 4) {
+        const f32x4 x = *(const f32x4*)(a.sv + at + e);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) vs[e + r] = x[r];
+      }
+    }
+  };
+  const auto load_scales = [&](int page, int j) {
+    if constexpr (H == 2) {
+      const int64_t at = place(page, j);
+#pragma unroll
+      for (int e = 0; e < R; e += 4) {
+        const f32x4 x = *(const f32x4*)(a.sk + at + e);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) ks[e + r] = x[r];
+      }
+    }
+  };
+
+  int step = step0 + wave;
+  if (step < step1) {
+    int jk = run_at(step, col >> 2), jv = run_at(step, g);
+    int pk = page_of(jk), pv = page_of(jv);
+    load_keys(pk, jk);
+    load_scales(pv, jv);
+    load_values(pv, jv);
+    int next = step + kWaves < step1 ? step + kWaves : step;
+    jk = run_at(next, col >> 2);
+    jv = run_at(next, g);
+    int pk2 = page_of(jk), pv2 = page_of(jv);
+    for (;; step += kWaves) {
+      const bool lost = pv < 0 || pv >= a.pages;       // this lane's run has no page
+      f32x4 sc[NT][NU];
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sc[t][u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int k = 0; k < KM; ++k) {
+          const kv_u32x4 x = operand<CT>(kw[u][k / H], k % H);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) sc[t][u] = mfma16<CT>(x, qf[t][k], sc[t][u]);
+        }
+      const bool more = step + kWaves < step1;
+      if (more) load_keys(pk2, jk);
+
+      // what a row does not see, and what is not a number behind its mask
+      const int t0 = step * TOK;
+      const bool edge = t0 + TOK > hi_first || t0 < lo_last || __any(lost);
+      uint32_t bad = 0;
+      if (edge) {
+#pragma unroll
+        for (int v = 0; v < VM; ++v)
+          if (16 * v < a.c.dim) bad |= drop_non_finite<CT>(vw[v]);
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) bad |= __shfl_xor(bad, d, 64);
+        if (lost) bad = 0xFFFFu;
+      }
+      kv_u32x4 pw[NT][H];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        float x[R];
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int e = 0; e < R; ++e) {
+          x[e] = sc[t][e >> 2][e & 3] * qs[t];
+          if constexpr (H == 2) x[e] *= ks[e];
+          if (edge) {
+            const int j = t0 + R * g + e;
+            x[e] = j < hi[t] && j >= lo[t]
+                       ? (bad >> e & 1 ? __builtin_nanf("") : x[e])
+                       : -__builtin_inff();
+          }
+          top = fmaxf(top, x[e]);
+        }
+        top = fmaxf(m[t], quarters_max(top));
+        float big = 0.0f;
+        if constexpr (H == 2) {
+#pragma unroll
+          for (int e = 0; e < R; ++e)
+            big = fmaxf(big, edge && x[e] == -__builtin_inff() ? 0.0f : vs[e]);
+          big = fmaxf(vref[t], quarters_max(big));
+        }
+        if (__any(top > m[t] || (H == 2 && big > vref[t]))) {
+          const float base = top == -__builtin_inff() ? 0.0f : top;
+          const float f = __builtin_amdgcn_exp2f(m[t] - base);
+          l[t] *= f;
+          const float fo = H == 2 ? (big > 0.0f ? f * (vref[t] / big) : 0.0f) : f;
+#pragma unroll
+          for (int v = 0; v < VM; ++v) o[t][v] *= fo;
+          m[t] = top;
+          vref[t] = big;
+        }
+        const float base = m[t] == -__builtin_inff() ? 0.0f : m[t];
+        const float unit_v = H == 2 && vref[t] > 0.0f ? 1.0f / vref[t] : 0.0f;
+        float w[R];
+#pragma unroll
+        for (int e = 0; e < R; ++e) {
+          const float p = __builtin_amdgcn_exp2f(x[e] - base);
+          l[t] += p;
+          w[e] = p;
+          if constexpr (H == 2)
+            w[e] = edge && x[e] == -__builtin_inff() ? 0.0f : p * (vs[e] * unit_v);
+        }
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+          pw[t][i] = kv_u32x4{pack2<CT>(w[8 * i], w[8 * i + 1]), pack2<CT>(w[8 * i + 2], w[8 * i + 3]),
+                              pack2<CT>(w[8 * i + 4], w[8 * i + 5]),
+                              pack2<CT>(w[8 * i + 6], w[8 * i + 7])};
+      }
+      if (more) load_scales(pv2, jv);
+#pragma unroll
+      for (int v = 0; v < VM; ++v)
+        if (16 * v < a.c.dim)
+#pragma unroll
+          for (int i = 0; i < H; ++i) {
+            const kv_u32x4 x = operand<CT>(vw[v], i);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) o[t][v] = mfma16<CT>(x, pw[t][i], o[t][v]);
+          }
+      if (!more) break;
+      load_values(pv2, jv);
+      pv = pv2;
+      next = step + 2 * kWaves < step1 ? step + 2 * kWaves : step + kWaves;
+      jk = run_at(next, col >> 2);
+      jv = run_at(next, g);
+      pk2 = page_of(jk);
+      pv2 = page_of(jv);
+    }
+  }
+
+  // the waves join: each scales its part to the largest maximum of a row
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    l[t] = quarters_sum(l[t]);
+    if (g == 0) {
+      stats[wave][16 * t + col][0] = m[t];
+      stats[wave][16 * t + col][1] = l[t];
+    }
+  }
+  __syncthreads();
+  float f[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stats[w][16 * t + col][0]);
+    f[t] = __builtin_amdgcn_exp2f(m[t] - (top == -__builtin_inff() ? 0.0f : top));
+    if (H == 2) f[t] *= vref[t];
+  }
+  const bool whole = s.parts == 1;
+  const int64_t part_row = ((int64_t)h * a.units + unit) * a.block_rows;
+  const int c4 = 4 * (threadIdx.x & 15);
+  for (int c0 = 0; c0 < a.c.dim; c0 += COLS) {
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < VM; ++v)
+      if (16 * v >= c0 && 16 * v < c0 + COLS)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          *(f32x4*)&joined[wave][16 * t + col][16 * v - c0 + 4 * g] = o[t][v] * f[t];
+    __syncthreads();
+    if (c0 + c4 >= a.c.dim) continue;
+    for (int r = threadIdx.x >> 4; r < rows; r += 16) {
+      f32x4 x = {0, 0, 0, 0};
+      float top = -__builtin_inff(), sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        x += *(const f32x4*)&joined[w][r][c4];
+        top = fmaxf(top, stats[w][r][0]);
+      }
+      const float base = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+        sum += stats[w][r][1] * __builtin_amdgcn_exp2f(stats[w][r][0] - base);
+      if (!whole) {
+        *(f32x4*)(a.part_o + (part_row + r) * a.c.dim + c0 + c4) = x;
+        if (c0 + c4 == 0) {
+          a.part_ml[2 * (part_row + r)] = top;
+          a.part_ml[2 * (part_row + r) + 1] = sum;
+        }
+        continue;
+      }
+      const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;     // a NaN sum stays one
+      x *= inv;
+      const int64_t t = s.first + (row0 + r) / a.group;
+      const int qh = h * a.group + (row0 + r) % a.group;
+      const bool half = a.type == LEECH_F16;
+      *(kv_u32x2*)(a.out + t * a.o_token + qh * a.o_head + c0 + c4) =
+          half ? kv_u32x2{pack2<kF16>(x[0], x[1]), pack2<kF16>(x[2], x[3])}
+               : kv_u32x2{pack2<kBf16>(x[0], x[1]), pack2<kBf16>(x[2], x[3])};
+      if (a.lse && c0 + c4 == 0)
+        a.lse[t * a.q_heads + qh] = sum != 0.0f ? (top + log2f(sum)) * kLn2 : -__builtin_inff();
+    }
+  }
+}
+
+// Joins the parts of one row (a token's query head), a wave a quarter of them.
+__global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a) {
+  __shared__ float acc[kWaves][kMaxHeadDim];
+  __shared__ float stats[kWaves][2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t t = blockIdx.x;
+  const int qh = blockIdx.y, h = qh / a.group;
+  Sequence s;
+  int b, u0;
+  if (!find(a, false, 0, t, &s, &b, &u0) || s.parts == 1) return;
+  const int row = (int)(t - s.first) * a.group + qh % a.group;
+  // (starts that do not ascend can number units that the launch did not hold)
+  if (u0 + (row / a.block_rows + 1) * s.parts > a.units) return;
+  const int64_t first = ((int64_t)h * a.units + u0 + row / a.block_rows * s.parts) * a.block_rows +
+                        row % a.block_rows;
+  float top = -__builtin_inff(), sum = 0.0f;
+  f32x4 x = {0, 0, 0, 0};
+  for (int p = wave; p < s.parts; p += kWaves) {
+    const int64_t at = first + (int64_t)p * a.block_rows;
+    const float pm = a.part_ml[2 * at], pl = a.part_ml[2 * at + 1];
+    f32x4 y = {0, 0, 0, 0};
+    if (4 * lane < a.c.dim) y = *(const f32x4*)(a.part_o + at * a.c.dim + 4 * lane);
+    const float most = fmaxf(top, pm), base = most == -__builtin_inff() ? 0.0f : most;
+    const float f0 = __builtin_amdgcn_exp2f(top - base), f1 = __builtin_amdgcn_exp2f(pm - base);
+    sum = sum * f0 + pl * f1;
+    x = x * f0 + y * f1;
+    top = most;
+  }
+  if (lane == 0) {
+    stats[wave][0] = top;
+    stats[wave][1] = sum;
+  }
+  if (4 * lane < a.c.dim) *(f32x4*)&acc[wave][4 * lane] = x;
+  __syncthreads();
+  float most = -__builtin_inff(), total = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) most = fmaxf(most, stats[w][0]);
+  const float base = most == -__builtin_inff() ? 0.0f : most;
+  float f[kWaves];
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    f[w] = __builtin_amdgcn_exp2f(stats[w][0] - base);
+    total += stats[w][1] * f[w];
+  }
+  const float inv = total != 0.0f ? 1.0f / total : 0.0f;
+  const int d = threadIdx.x;
+  if (d < a.c.dim) {
+    float y = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) y += acc[w][d] * f[w];
+    y *= inv;
+    a.out[t * a.o_token + qh * a.o_head + d] =
+        (uint16_t)(a.type == LEECH_F16 ? half_bits(y) : bf16_bits(y));
+  }
+  if (a.lse && d == 0)
+    a.lse[t * a.q_heads + qh] = total != 0.0f ? (most + log2f(total)) * kLn2 : -__builtin_inff();
 }
 
 // ------------------------------------------------------------------ host side
+constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;
+constexpr int kTarget = 1024;          // workgroups that split sequences come to
+constexpr int kMinTokens = 256;        // keys of a part, at least
+
+// How a call is cut: a function of sizes alone.
+struct Cut {
+  int nt, block_rows, log_step, min_steps, split;
+  int64_t units;
+  size_t bytes;
+};
+
+int cut(const leech_attend_args* g, const CacheShape& c, Cut* out) {
+  const int64_t group = g->q_heads / c.heads;
+  const int64_t rows = std::min<int64_t>(g->max_new, g->T) * group;
+  Cut k;
+  k.nt = rows > 16 ? 2 : 1;
+  k.block_rows = 16 * k.nt;
+  k.log_step = type_bytes(c.type) == 2 ? 5 : 6;
+  k.min_steps = kMinTokens >> k.log_step;
+  const int64_t live = std::min<int64_t>(g->B, g->T);
+  const int64_t tiles = g->T * group / k.block_rows + live;
+  const int64_t keys = (int64_t)g->table_pages << c.log_page;
+  k.split = keys > kMinTokens && (g->T * group / k.block_rows) * c.heads < kTarget;
+  // (two more for the roundings of the plan's f32 total)
+  k.units = tiles + (k.split ? (kTarget + c.heads - 1) / c.heads + 2 : 0);
+  if (k.units * c.heads * 64 * kWaves > kMaxThreads)
+    return set_error(LEECH_E_SHAPE, "too many rows for a launch");
+  k.bytes = k.split ? (size_t)(c.heads * k.units * k.block_rows) * (c.dim + 2) * sizeof(float) : 0;
+  *out = k;
+  return LEECH_OK;
+}
+
 // Sizes alone: what the workspace goes by.
-int check_sizes(const leech_kv_cache* cache, const leech_attend_args* g, CacheShape* shape) {
+int check_sizes(const leech_kv_cache* cache, const leech_attend_args* g, CacheShape* shape,
+                Cut* k) {
   const int rc = check_cache(cache, shape);
   if (rc) return rc;
   if (!g) return set_error(LEECH_E_ARG, "the arguments are NULL");
@@ -131,13 +688,13 @@ int check_sizes(const leech_kv_cache* cache, const leech_attend_args* g, CacheSh
     return set_error(LEECH_E_ARG, "a 16-bit cache must have the queries' type");
   if (g->q_heads <= 0 || g->q_heads > 65535 || g->q_heads % cache->heads)
     return set_error(LEECH_E_SHAPE, "query heads must be a multiple of the cache's, up to 65535");
-  if (g->T < 0 || g->T > 0x7fffffff || g->B < 0 || g->max_new < 0)
-    return set_error(LEECH_E_SHAPE, "T, B and max_new must be 0 to 2^31 - 1");
-  if (g->table_pages < 0 || ((int64_t)g->table_pages << shape->log_page) > 0x7fffffff)
-    return set_error(LEECH_E_SHAPE, "a row of the page table holds at most 2^31 - 1 tokens");
+  if (g->T < 0 || g->B < 0 || g->max_new < 0 || g->T * g->q_heads > 0x7fffffff)
+    return set_error(LEECH_E_SHAPE, "B and max_new must not be negative, T · q_heads 0 to 2^31 - 1");
+  if (g->table_pages < 0 || ((int64_t)g->table_pages << shape->log_page) > 0x7fffff00)
+    return set_error(LEECH_E_SHAPE, "a row of the page table holds fewer than 2^31 - 256 tokens");
   if (!g->q_start && g->T != g->B)
     return set_error(LEECH_E_SHAPE, "without q_start there is one new token a sequence");
-  return LEECH_OK;
+  return cut(g, *shape, k);
 }
 
 int check_strides(const char* name, const void* p, int64_t token, int64_t head) {
@@ -146,6 +703,14 @@ int check_strides(const char* name, const void* p, int64_t token, int64_t head) 
     return set_error(LEECH_E_ARG, std::string(name) +
                                       ": needs 16-byte alignment and strides of 8 elements");
   return LEECH_OK;
+}
+
+typedef void (*AttendFn)(AttendArgs);
+template <int CT>
+AttendFn pick(int dim, int nt) {
+  if (dim <= 64) return nt == 1 ? stream_kernel<CT, 64, 1> : stream_kernel<CT, 64, 2>;
+  if (dim <= 128) return nt == 1 ? stream_kernel<CT, 128, 1> : stream_kernel<CT, 128, 2>;
+  return nt == 1 ? stream_kernel<CT, 256, 1> : stream_kernel<CT, 256, 2>;
 }
 
 }  // namespace
@@ -157,10 +722,11 @@ extern "C" int leech_attend_workspace(const leech_kv_cache* cache, const leech_a
                                       size_t* bytes) {
   clear_error();
   CacheShape shape;
-  const int rc = check_sizes(cache, args, &shape);
+  Cut k;
+  const int rc = check_sizes(cache, args, &shape, &k);
   if (rc) return rc;
   if (!bytes) return set_error(LEECH_E_ARG, "bytes is NULL");
-  *bytes = 0;
+  *bytes = k.bytes;
   return LEECH_OK;
 }
 
@@ -168,7 +734,8 @@ extern "C" int leech_attend(const leech_kv_cache* cache, const leech_attend_args
                             void* stream) {
   clear_error();
   AttendArgs a = {};
-  int rc = check_sizes(cache, g, &a.c);
+  Cut k;
+  int rc = check_sizes(cache, g, &a.c, &k);
   if (rc) return rc;
   if ((g->causal != 0 && g->causal != 1) || g->window < 0)
     return set_error(LEECH_E_ARG, "causal must be 0 or 1 and window not negative");
@@ -185,6 +752,9 @@ extern "C" int leech_attend(const leech_kv_cache* cache, const leech_attend_args
   if (((uintptr_t)g->q_start & 3) || ((uintptr_t)g->kv_len & 3) || ((uintptr_t)g->page_table & 3) ||
       ((uintptr_t)g->lse & 3))
     return set_error(LEECH_E_ARG, "misaligned device pointer");
+  if (k.bytes && (!g->workspace || g->workspace_bytes < k.bytes || ((uintptr_t)g->workspace & 15)))
+    return set_error(LEECH_E_ARG, "the workspace is NULL, misaligned or smaller than "
+                                  "leech_attend_workspace says");
   a.ck = (const uint8_t*)cache->k;
   a.cv = (const uint8_t*)cache->v;
   a.sk = cache->k_scale;
@@ -210,9 +780,26 @@ extern "C" int leech_attend(const leech_kv_cache* cache, const leech_attend_args
   a.max_new = g->max_new;
   a.causal = g->causal;
   a.window = g->window;
-  a.scale = g->scale;
-  hipLaunchKernelGGL(attend_kernel, dim3((unsigned)a.T, (unsigned)a.q_heads), dim3(64), 0,
+  a.scale = g->scale * kLog2e;
+  a.block_rows = k.block_rows;
+  a.log_step = k.log_step;
+  a.min_steps = k.min_steps;
+  a.units = (int32_t)k.units;
+  a.split = k.split;
+  a.target = kTarget;
+  a.part_o = (float*)g->workspace;
+  a.part_ml = a.part_o + (int64_t)a.c.heads * k.units * k.block_rows * a.c.dim;
+  AttendFn fn = cache->type == LEECH_F16    ? pick<kF16>(cache->dim, k.nt)
+                : cache->type == LEECH_BF16 ? pick<kBf16>(cache->dim, k.nt)
+                : cache->type == LEECH_INT8 ? pick<kInt8>(cache->dim, k.nt)
+                                            : pick<kE4m3>(cache->dim, k.nt);
+  hipLaunchKernelGGL(fn, dim3((unsigned)(a.c.heads * k.units)), dim3(64 * kWaves), 0,
                      (hipStream_t)stream, a);
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? LEECH_OK : hip_fail("attend launch", e);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return hip_fail("attend launch", e);
+  if (!k.split) return LEECH_OK;
+  hipLaunchKernelGGL(join_kernel, dim3((unsigned)a.T, (unsigned)a.q_heads), dim3(64 * kWaves), 0,
+                     (hipStream_t)stream, a);
+  e = hipGetLastError();
+  return e == hipSuccess ? LEECH_OK : hip_fail("attend join launch", e);
 }

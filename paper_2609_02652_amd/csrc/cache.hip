@@ -565,9 +565,9 @@ int check_cache(const leech_kv_cache* c, CacheShape* shape) {
     return set_error(LEECH_E_SHAPE, "a page must hold a power of two of tokens, 16 to 65536");
   if (c->pages <= 0 || c->pages > 0x7fffffff)
     return set_error(LEECH_E_SHAPE, "a cache needs 1 to 2^31 - 1 pages");
-  if (((uintptr_t)c->k & 15) || ((uintptr_t)c->v & 15) || ((uintptr_t)c->k_scale & 3) ||
-      ((uintptr_t)c->v_scale & 3))
-    return set_error(LEECH_E_ARG, "misaligned cache pointer (keys and values: 16 bytes)");
+  if (((uintptr_t)c->k & 15) || ((uintptr_t)c->v & 15) || ((uintptr_t)c->k_scale & 15) ||
+      ((uintptr_t)c->v_scale & 15))
+    return set_error(LEECH_E_ARG, "a cache's pointers must be 16-byte aligned");
   int log_page = 4;
   while (1 << log_page < c->page_size) ++log_page;
   *shape = {c->pages * c->page_size, c->heads, c->dim, log_page, c->type};

@@ -13,7 +13,9 @@ rounded to nearest; f32 2^-24):
              the scale), and what the rotation was off by
   attention  the weights are rounded to q's type, u each: u Σ p |v| (a weight
              under f16's normal range is off by 2^-25 of the largest: with it
-             2^-25 Σ over the tokens of the largest |v|); a score's f32 error e_s
+             2^-25 Σ over the tokens of the largest |v|; so too for bf16 queries over
+             8-bit codes, whose weights, times the value's scale over the largest
+             scale seen, are f16); a score's f32 error e_s
              = (dim + 8) 2^-24 Σ |q k| scale + 2^-21 moves out by 2 e_s Σ p |v|
              and lse by e_s; then one rounding of out.  A weight under f32's normal
              range (or out, 8 bits of exponent too) may be lost whole: 2^-126 for
@@ -359,7 +361,7 @@ class Batch:
                     np.abs(q[:, h]) @ np.abs(kh).T).max(1) + 2.0 ** -21
                 bound = (U[kind] + 2 * es)[:, None] * av + U[kind] * np.abs(want[:, h])
                 bound += (length + 1) * 2.0 ** -126 * (1 + np.abs(v[:, h // group]).max())
-                if kind == "f16":
+                if kind == "f16" or self.cache.k_scale is not None:
                     bound += 2.0 ** -25 * ((w[:, h] > 0).sum(1) / np.maximum(
                         (w[:, h] / w[:, h].max(1, keepdims=True).clip(1e-300)).sum(1), 1.0)
                         * np.abs(v[:, h // group]).max())[:, None] + 2.0 ** -25

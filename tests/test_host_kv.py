@@ -120,7 +120,7 @@ def attend_args(**kw):
 @pytest.mark.parametrize("kw,code", [
     (dict(type=_lib.F32), ARG), (dict(type=_lib.INT8), ARG), (dict(q_heads=3), SHAPE),
     (dict(q_heads=0), SHAPE), (dict(T=-1), SHAPE), (dict(T=1 << 31), SHAPE), (dict(B=-1), SHAPE),
-    (dict(max_new=-1), SHAPE), (dict(table_pages=-1), SHAPE), (dict(table_pages=1 << 27), SHAPE),
+    (dict(max_new=-1), SHAPE), (dict(table_pages=-1), SHAPE), (dict(table_pages=1 << 26), SHAPE),
     (dict(q_start=None), SHAPE), (dict(causal=2), ARG), (dict(window=-1), ARG),
     (dict(scale=math.inf), ARG), (dict(scale=math.nan), ARG), (dict(q=None), ARG),
     (dict(out=None), ARG), (dict(q=FAKE + 8), ARG), (dict(q_head_stride=60), ARG),
@@ -137,6 +137,15 @@ def test_attend_refuses_mixed_16_bit_types_and_no_arguments():
     refused(ARG, _lib.attend, None, attend_args())
     for kw in (dict(T=0), dict(B=0), dict(max_new=0)):      # nothing to do
         _lib.attend(cache(), attend_args(**kw))
+
+
+def test_attend_refuses_a_workspace_that_is_too_small():
+    args = attend_args(T=2, q_start=None, max_new=1, table_pages=1 << 16)
+    need = _lib.attend_workspace(cache(), args)
+    assert need > 0
+    for p, n in ((None, need), (FAKE, need - 1), (FAKE + 4, need)):
+        args.workspace, args.workspace_bytes = p, n
+        refused(ARG, _lib.attend, cache(), args)
 
 
 def test_the_python_calls_refuse_host_tensors_and_wrong_shapes():
