@@ -47,8 +47,9 @@ struct AttendArgs {
   int64_t T, pages;
   int32_t type, q_heads, group, B, table_pages, max_new, causal, window;
   float scale;                // times log2 e
-  // how the work is cut (see Plan)
+  // how the work is cut (see the plan)
   int32_t block_rows, log_step, min_steps, units, split;
+  int32_t over, upto;         // sequences of over < rows <= upto are this launch's
   float target;
   float *part_o, *part_ml;    // [head][unit][row][dim], [head][unit][row][2]
 };
@@ -77,6 +78,7 @@ __device__ __forceinline__ Sequence sequence(const AttendArgs& a, int b) {
   const int64_t n = start_of(a, b + 1) - s.first;
   s.n = n < 0 ? 0 : (int32_t)n;
   s.rows = (s.n < a.max_new ? s.n : a.max_new) * a.group;
+  if (s.rows <= a.over || s.rows > a.upto) return s;
   s.tiles = (s.rows + a.block_rows - 1) / a.block_rows;
   const int64_t room = (int64_t)a.table_pages << a.c.log_page;
   const int32_t len = a.kv_len[b];
@@ -123,7 +125,8 @@ __device__ __forceinline__ bool find(const AttendArgs& a, bool by_unit, int unit
     s.parts = a.split ? (s.steps + steps - 1) / steps : 1;
     const int own = s.tiles * s.parts, upto = before + wave_scan(own);
     const bool hit = by_unit ? unit >= upto - own && unit < upto
-                             : token >= s.first && token - s.first < (s.n < a.max_new ? s.n : a.max_new);
+                             : s.tiles && token >= s.first &&
+                                   token - s.first < (s.n < a.max_new ? s.n : a.max_new);
     const uint64_t mask = __ballot(hit);
     if (mask) {
       const int at = __ffsll((unsigned long long)mask) - 1;
@@ -263,6 +266,35 @@ __device__ __forceinline__ uint32_t drop_non_finite(kv_u32x4& w) {
   return bad;
 }
 
+// A query's bf16 operands (its lanes: those that differ by WIDTH / 2, and by 32) to
+// f16, the row's largest just below 2^15: what falls under f16's range there is
+// under 2^-39 of the largest.  Returns scale times the power of two taken out.
+template <int KM, int WIDTH>
+__device__ __forceinline__ float to_f16(kv_u32x4* q, float scale) {
+  float big = 0.0f;
+#pragma unroll
+  for (int m = 0; m < KM; ++m)
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      big = fmaxf(big, __builtin_fabsf(bf16_value(q[m][e >> 1] >> (16 * (e & 1)) & 0xFFFFu)));
+  if constexpr (WIDTH == 32) {
+    big = quarters_max(big);
+  } else {
+    const Pair p = swapped<64>(big);
+    big = fmaxf(p.a, p.b);
+  }
+  int ex = (int)(__builtin_bit_cast(uint32_t, big) >> 23 & 0xFF) - 127 - 14;
+  ex = big > 0.0f && big < __builtin_inff() ? ex : 0;
+#pragma unroll
+  for (int m = 0; m < KM; ++m)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t w = q[m][e];
+      q[m][e] = pack2<kF16>(ldexpf(bf16_value(w & 0xFFFFu), -ex), ldexpf(bf16_value(w >> 16), -ex));
+    }
+  return ldexpf(scale, ex);
+}
+
 constexpr int kWaves = 4;
 
 // A workgroup is a unit of up to 16·NT rows; its waves take the unit's steps in
@@ -318,28 +350,7 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(AttendArgs a) {
       qf[t][m] = in && d < a.c.dim ? *(const kv_u32x4*)(q + d) : kv_u32x4{0, 0, 0, 0};
     }
     qs[t] = a.scale;
-    if (H == 2 && a.type == LEECH_BF16) {
-      // to f16, the row's largest just below 2^15: what falls under f16's range
-      // there is under 2^-39 of the largest
-      float big = 0.0f;
-#pragma unroll
-      for (int m = 0; m < KM; ++m)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          big = fmaxf(big, __builtin_fabsf(bf16_value(qf[t][m][e >> 1] >> (16 * (e & 1)) & 0xFFFFu)));
-      big = quarters_max(big);
-      int ex = (int)(__builtin_bit_cast(uint32_t, big) >> 23 & 0xFF) - 127 - 14;
-      ex = big > 0.0f && big < __builtin_inff() ? ex : 0;
-#pragma unroll
-      for (int m = 0; m < KM; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t w = qf[t][m][e];
-          qf[t][m][e] = pack2<kF16>(ldexpf(bf16_value(w & 0xFFFFu), -ex),
-                                    ldexpf(bf16_value(w >> 16), -ex));
-        }
-      qs[t] = ldexpf(a.scale, ex);
-    }
+    if (H == 2 && a.type == LEECH_BF16) qs[t] = to_f16<KM, 32>(qf[t], a.scale);
   }
 
   f32x4 o[NT][VM];
@@ -585,6 +596,323 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(AttendArgs a) {
   }
 }
 
+// ------------------------------------------------------------- many rows at once
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <int CT>
+__device__ __forceinline__ f32x16 mfma32(kv_u32x4 a, kv_u32x4 b, f32x16 c) {
+  if constexpr (CT == kBf16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+constexpr int kTileRows = 32 * kWaves;
+template <int DT>
+constexpr int kTileTokens = DT > 128 ? 32 : 64;
+
+// LDS of the tile kernel: two buffers of keys and values (as the products take
+// them, two bytes an element), of their scales, then for three tiles which
+// tokens' values are not finite, and for four where their tokens lie.
+template <int CT, int DT>
+struct TileLds {
+  static constexpr int TOK = kTileTokens<DT>;
+  kv_u32x4 k[2][TOK * DT / 8];
+  kv_u32x4 v[2][TOK * DT / 8];
+  float ks[2][TOK], vs[2][TOK];
+  uint32_t bad[3][TOK / 8];
+  int64_t where[4][TOK / 16];       // slot of each sixteen tokens, -1: no such page
+};
+
+// A workgroup is a unit of up to 128 rows, a wave 32 of them; all share the keys
+// and values, which go through LDS a tile of 64 (32 at DT = 256) tokens at a time:
+// the next tile's sixteen-byte loads are under way while this one is worked on,
+// widened to 16 bits on their way if they are codes.  Products are 32×32×16,
+// transposed as in stream_kernel: row m of a 32-token key tile is token 16·(m / 16)
+// + 8·(m / 4 % 2) + 4·(m / 8 % 2) + m % 4, so that a lane's scores are of whole
+// runs of eight tokens, those whose values it multiplies next.  Keys lie in LDS
+// row by row, chunk c of row r in place c ^ r % 16 (as far as a row has places),
+// which puts the chunks that a read takes at once in different banks.
+template <int CT, int DT>
+__global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(AttendArgs a) {
+  constexpr int TOK = kTileTokens<DT>, S = kBytes<CT>, R = kRun<CT>;
+  constexpr int NK = TOK / 32;                 // key tiles of 32
+  constexpr int KM = DT / 16;                  // products along a head
+  constexpr int VM = DT / 32;                  // tiles of coordinates
+  constexpr int CH = DT / 8;                   // LDS chunks of a key row
+  constexpr int SWZ = CH < 16 ? CH - 1 : 15;
+  constexpr int LC = DT * S / 16;              // sixteen-byte loads of a key row
+  constexpr int NL = TOK * LC / (64 * kWaves); // of a thread, for keys; as many for values
+  constexpr bool CODES = S == 1;
+  extern __shared__ __attribute__((aligned(16))) uint8_t raw[];
+  TileLds<CT, DT>& lds = *reinterpret_cast<TileLds<CT, DT>*>(raw);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int h = blockIdx.x % a.c.heads, unit = blockIdx.x / a.c.heads;
+  Sequence s;
+  int b, u0;
+  if (!find(a, true, unit, 0, &s, &b, &u0)) return;
+  // (starts that do not ascend can number units that the workspace does not hold)
+  if (s.parts > 1 && u0 + s.tiles * s.parts > a.units) return;
+  // the tiles that see most keys first: they run longest
+  const int tile = s.tiles - 1 - (unit - u0) / s.parts, part = (unit - u0) % s.parts;
+  const int row0 = tile * kTileRows;
+  const int rows = s.rows - row0 < kTileRows ? s.rows - row0 : kTileRows;
+  const int col = lane & 31, half = lane >> 5;
+
+  int lo_first, hi_first, lo_last, hi_last;
+  row_range(a, s, row0, lo_first, hi_first);
+  row_range(a, s, row0 + rows - 1, lo_last, hi_last);
+  int step0 = lo_first / TOK, step1 = (hi_last + TOK - 1) / TOK;
+  if (step1 < step0) step1 = step0;
+  const int64_t span = step1 - step0;
+  step1 = step0 + (int)(span * (part + 1) / s.parts);
+  step0 = step0 + (int)(span * part / s.parts);
+
+  // this wave's rows, and the keys that they see
+  const int wrow = 32 * wave, r = row0 + wrow + col;
+  const bool in = wrow + col < rows, live = wrow < rows;
+  int lo = 0, hi = 0, wlo = 0, whi = 0, wlo_last = 0, whi_first = 0;
+  if (live) {
+    const int last = rows - wrow < 32 ? rows - 1 : wrow + 31;
+    row_range(a, s, row0 + wrow, wlo, whi_first);
+    row_range(a, s, row0 + last, wlo_last, whi);
+  }
+  if (in) row_range(a, s, r, lo, hi);
+  kv_u32x4 qf[KM];
+  const uint16_t* q = a.q + (s.first + r / a.group) * a.q_token +
+                      ((int64_t)h * a.group + r % a.group) * a.q_head;
+#pragma unroll
+  for (int m = 0; m < KM; ++m) {
+    const int d = 16 * m + 8 * half;
+    qf[m] = in && d < a.c.dim ? *(const kv_u32x4*)(q + d) : kv_u32x4{0, 0, 0, 0};
+  }
+  float qs = a.scale;
+  if (CODES && a.type == LEECH_BF16) qs = to_f16<KM, 64>(qf, a.scale);
+
+  f32x16 o[VM];
+#pragma unroll
+  for (int v = 0; v < VM; ++v)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[v][e] = 0.0f;
+  float m = -__builtin_inff(), l = 0.0f, vref = 0.0f;
+
+  const int row_bytes = a.c.dim * S;
+  const int32_t* table = a.table + b * a.table_stride;
+  const int first16 = lo_first & ~15, last16 = (hi_last - 1) & ~15;
+  const auto slot16 = [&](int step, int i) {       // of sixteen tokens, clamped to those seen
+    int j = step * TOK + 16 * i;
+    j = j < first16 ? first16 : j > last16 ? last16 : j;
+    const int p = table[j >> a.c.log_page];
+    return p < 0 || p >= a.pages ? (int64_t)-1
+                                 : (((int64_t)p * a.c.heads + h) << a.c.log_page) +
+                                       (j & ((1 << a.c.log_page) - 1));
+  };
+  kv_u32x4 kw[NL], vw[NL];
+  float sc = 0.0f;
+  const auto load = [&](int step) {
+    const int64_t* where = lds.where[step & 3];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int at = i * 64 * kWaves + tid, t = at / LC, c = at % LC;
+      const int64_t w = where[t >> 4];
+      kw[i] = w >= 0 && 16 * c < row_bytes
+                  ? *(const kv_u32x4*)(a.ck + (w + (t & 15)) * row_bytes + 16 * c)
+                  : kv_u32x4{0, 0, 0, 0};
+      const int run = at / DT, d = at % DT;
+      const int64_t x = where[run * R >> 4];
+      vw[i] = x >= 0 && d < a.c.dim
+                  ? *(const kv_u32x4*)(a.cv + (x + (run * R & 15)) * row_bytes + 16 * d)
+                  : kv_u32x4{0, 0, 0, 0};
+    }
+    if constexpr (CODES) {
+      const int t = tid & (TOK - 1);
+      const int64_t w = where[t >> 4];
+      if (tid < 2 * TOK && w >= 0) sc = (tid < TOK ? a.sk : a.sv)[w + (t & 15)];
+    }
+  };
+  const auto keep = [&](int step) {
+    const int buf = step & 1;
+    const bool edge = step * TOK + TOK > hi_first || step * TOK < lo_last;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int at = i * 64 * kWaves + tid, t = at / LC, c = at % LC;
+      const int run = at / DT, d = at % DT;
+      if constexpr (CODES) {
+        lds.k[buf][t * CH + (2 * c ^ (t & SWZ))] = operand<CT>(kw[i], 0);
+        lds.k[buf][t * CH + (2 * c + 1 ^ (t & SWZ))] = operand<CT>(kw[i], 1);
+      } else {
+        lds.k[buf][t * CH + (c ^ (t & SWZ))] = kw[i];
+      }
+      // values behind some row's mask must be numbers; a token that has none
+      // counts as NaN for the rows that see it
+      const bool lost = lds.where[step & 3][run * R >> 4] < 0;
+      uint32_t bad = 0;
+      if (edge) bad = drop_non_finite<CT>(vw[i]);
+      if (lost) bad = 0xFFFFu;
+      if constexpr (CODES) {
+        lds.v[buf][2 * run * DT + d] = operand<CT>(vw[i], 0);
+        lds.v[buf][(2 * run + 1) * DT + d] = operand<CT>(vw[i], 1);
+        if (bad) {
+          atomicOr(&lds.bad[step % 3][2 * run], bad & 0xFFu);
+          atomicOr(&lds.bad[step % 3][2 * run + 1], bad >> 8);
+        }
+      } else {
+        lds.v[buf][run * DT + d] = vw[i];
+        if (bad) atomicOr(&lds.bad[step % 3][run], bad & 0xFFu);
+      }
+    }
+    if constexpr (CODES)
+      if (tid < 2 * TOK) (tid < TOK ? lds.ks : lds.vs)[buf][tid & (TOK - 1)] = sc;
+  };
+
+  if (step0 < step1) {
+    if (tid < TOK / 16) {
+      lds.where[step0 & 3][tid] = slot16(step0, tid);
+      lds.where[(step0 + 1) & 3][tid] = slot16(step0 + 1, tid);
+    }
+    if (tid < TOK / 8) lds.bad[0][tid] = lds.bad[1][tid] = lds.bad[2][tid] = 0;
+    __syncthreads();
+    load(step0);
+    keep(step0);
+    __syncthreads();
+  }
+  for (int step = step0; step < step1; ++step) {
+    const int buf = step & 1, t0 = step * TOK;
+    const bool more = step + 1 < step1;
+    int64_t ahead = 0;
+    if (more) {
+      load(step + 1);
+      if (tid < TOK / 16) ahead = slot16(step + 2, tid);
+      if (tid < TOK / 8) lds.bad[(step + 2) % 3][tid] = 0;
+    }
+    if (live && t0 < whi && t0 + TOK > wlo) {
+      f32x16 sc32[NK];
+#pragma unroll
+      for (int n = 0; n < NK; ++n) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc32[n][e] = 0.0f;
+        const int t = 32 * n + 16 * (col >> 4) + 8 * (col >> 2 & 1) + 4 * (col >> 3 & 1) + (col & 3);
+#pragma unroll
+        for (int k = 0; k < KM; ++k)
+          sc32[n] = mfma32<CT>(lds.k[buf][t * CH + (2 * k + half ^ (t & SWZ))], qf[k], sc32[n]);
+      }
+      // score e of tile n: token 32 n + 16 (e / 8) + 8 half + e % 8
+      uint32_t bad = 0;
+#pragma unroll
+      for (int n = 0; n < 2 * NK; ++n) bad |= lds.bad[step % 3][2 * n + half] << (8 * n);
+      const bool edge = t0 + TOK > whi_first || t0 < wlo_last || __any(bad != 0);
+      float top = -__builtin_inff(), big = 0.0f;
+#pragma unroll
+      for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float x = sc32[n][e] * qs;
+          const int j = 32 * n + 16 * (e >> 3) + 8 * half + (e & 7);
+          if constexpr (CODES) x *= lds.ks[buf][j];
+          if (edge) {
+            const bool sees = t0 + j < hi && t0 + j >= lo;
+            x = sees ? (bad >> (16 * n + e) & 1 ? __builtin_nanf("") : x) : -__builtin_inff();
+            if constexpr (CODES)
+              if (sees) big = fmaxf(big, lds.vs[buf][j]);
+          } else if constexpr (CODES) {
+            big = fmaxf(big, lds.vs[buf][j]);
+          }
+          sc32[n][e] = x;
+          top = fmaxf(top, x);
+        }
+      Pair p = swapped<64>(top);
+      top = fmaxf(m, fmaxf(p.a, p.b));
+      if constexpr (CODES) {
+        p = swapped<64>(big);
+        big = fmaxf(vref, fmaxf(p.a, p.b));
+      }
+      if (__any(top > m || (CODES && big > vref))) {
+        const float f = __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.0f : top));
+        l *= f;
+        const float fo = CODES ? (big > 0.0f ? f * (vref / big) : 0.0f) : f;
+#pragma unroll
+        for (int v = 0; v < VM; ++v) o[v] *= fo;
+        m = top;
+        vref = big;
+      }
+      const float base = m == -__builtin_inff() ? 0.0f : m;
+      const float unit_v = CODES && vref > 0.0f ? 1.0f / vref : 0.0f;
+      kv_u32x4 pw[2 * NK];
+#pragma unroll
+      for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          float w[2];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const float x = sc32[n][e + y];
+            const float pe = __builtin_amdgcn_exp2f(x - base);
+            l += pe;
+            w[y] = pe;
+            if constexpr (CODES) {
+              const int j = 32 * n + 16 * (e >> 3) + 8 * half + (e & 7) + y;
+              w[y] = edge && x == -__builtin_inff() ? 0.0f : pe * (lds.vs[buf][j] * unit_v);
+            }
+          }
+          pw[2 * n + (e >> 3)][(e & 7) >> 1] = pack2<CT>(w[0], w[1]);
+        }
+#pragma unroll
+      for (int n = 0; n < 2 * NK; ++n)
+#pragma unroll
+        for (int v = 0; v < VM; ++v)
+          o[v] = mfma32<CT>(lds.v[buf][(2 * n + half) * DT + 32 * v + col], pw[n], o[v]);
+    }
+    if (more) {
+      keep(step + 1);
+      if (tid < TOK / 16) lds.where[(step + 2) & 3][tid] = ahead;
+    }
+    __syncthreads();
+  }
+
+  Pair p = swapped<64>(l);
+  l = p.a + p.b;
+  if (!in) return;
+  const float fv = CODES ? vref : 1.0f;
+  if (s.parts > 1) {
+    const int64_t at = ((int64_t)h * a.units + u0 + tile * s.parts + part) * kTileRows + wrow + col;
+#pragma unroll
+    for (int v = 0; v < VM; ++v)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int d = 32 * v + 8 * i + 4 * half;
+        if (d < a.c.dim)
+          *(f32x4*)(a.part_o + at * a.c.dim + d) =
+              f32x4{o[v][4 * i], o[v][4 * i + 1], o[v][4 * i + 2], o[v][4 * i + 3]} * fv;
+      }
+    if (half == 0) {
+      a.part_ml[2 * at] = m;
+      a.part_ml[2 * at + 1] = l;
+    }
+    return;
+  }
+  const float inv = (l != 0.0f ? 1.0f / l : 0.0f) * fv;
+  const int64_t t = s.first + r / a.group;
+  const int qh = h * a.group + r % a.group;
+  uint16_t* out = a.out + t * a.o_token + qh * a.o_head;
+#pragma unroll
+  for (int v = 0; v < VM; ++v)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int d = 32 * v + 8 * i + 4 * half;
+      if (d >= a.c.dim) continue;
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = o[v][4 * i + e] * inv;
+      *(kv_u32x2*)(out + d) = a.type == LEECH_F16
+                                  ? kv_u32x2{pack2<kF16>(x[0], x[1]), pack2<kF16>(x[2], x[3])}
+                                  : kv_u32x2{pack2<kBf16>(x[0], x[1]), pack2<kBf16>(x[2], x[3])};
+    }
+  if (a.lse && half == 0)
+    a.lse[t * a.q_heads + qh] = l != 0.0f ? (m + log2f(l)) * kLn2 : -__builtin_inff();
+}
+
 // Joins the parts of one row (a token's query head), a wave a quarter of them.
 __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a) {
   __shared__ float acc[kWaves][kMaxHeadDim];
@@ -645,40 +973,66 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a) {
 
 // ------------------------------------------------------------------ host side
 constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;
-constexpr int kTarget = 1024;          // workgroups that split sequences come to
+constexpr int kFewRows = 32;           // rows of a sequence that stream_kernel takes
+constexpr int kTargetFew = 1024, kTargetMany = 512;   // workgroups that split sequences come to
 constexpr int kMinTokens = 256;        // keys of a part, at least
 
-// How a call is cut: a function of sizes alone.
+// One launch's share of a call: a function of sizes alone.
 struct Cut {
-  int nt, block_rows, log_step, min_steps, split;
+  int block_rows, log_step, min_steps, split, over, upto, target;
   int64_t units;
   size_t bytes;
 };
+struct Cuts {
+  Cut few, many;                       // units = 0: not launched
+};
 
-int cut(const leech_attend_args* g, const CacheShape& c, Cut* out) {
+int cut(const leech_attend_args* g, const CacheShape& c, bool many, Cut* k) {
+  const int64_t group = g->q_heads / c.heads, T = g->T * group;
+  const int64_t keys = (int64_t)g->table_pages << c.log_page;
+  k->target = many ? kTargetMany : kTargetFew;
+  k->log_step = many ? (c.dim > 128 ? 5 : 6) : type_bytes(c.type) == 2 ? 5 : 6;
+  k->min_steps = kMinTokens >> k->log_step;
+  const int64_t least = (T + k->block_rows - 1) / k->block_rows;
+  k->split = keys > kMinTokens && least * c.heads < k->target;
+  // (two more for the roundings of the plan's f32 total)
+  k->units = T / k->block_rows + std::min<int64_t>(g->B, g->T) +
+             (k->split ? (k->target + c.heads - 1) / c.heads + 2 : 0);
+  if (k->units * c.heads * 64 * kWaves > kMaxThreads)
+    return set_error(LEECH_E_SHAPE, "too many rows for a launch");
+  k->bytes = k->split ? (size_t)(c.heads * k->units * k->block_rows) * (c.dim + 2) * sizeof(float)
+                      : 0;
+  return LEECH_OK;
+}
+
+// Sequences of up to kFewRows rows are stream_kernel's; tile_kernel takes longer
+// ones, and all of them where no sequence need be short (T rows make B sequences
+// of max_new).
+int cut_all(const leech_attend_args* g, const CacheShape& c, Cuts* k) {
   const int64_t group = g->q_heads / c.heads;
   const int64_t rows = std::min<int64_t>(g->max_new, g->T) * group;
-  Cut k;
-  k.nt = rows > 16 ? 2 : 1;
-  k.block_rows = 16 * k.nt;
-  k.log_step = type_bytes(c.type) == 2 ? 5 : 6;
-  k.min_steps = kMinTokens >> k.log_step;
-  const int64_t live = std::min<int64_t>(g->B, g->T);
-  const int64_t tiles = g->T * group / k.block_rows + live;
-  const int64_t keys = (int64_t)g->table_pages << c.log_page;
-  k.split = keys > kMinTokens && (g->T * group / k.block_rows) * c.heads < kTarget;
-  // (two more for the roundings of the plan's f32 total)
-  k.units = tiles + (k.split ? (kTarget + c.heads - 1) / c.heads + 2 : 0);
-  if (k.units * c.heads * 64 * kWaves > kMaxThreads)
-    return set_error(LEECH_E_SHAPE, "too many rows for a launch");
-  k.bytes = k.split ? (size_t)(c.heads * k.units * k.block_rows) * (c.dim + 2) * sizeof(float) : 0;
-  *out = k;
-  return LEECH_OK;
+  *k = {};
+  int rc = LEECH_OK;
+  const bool many = rows > kFewRows;
+  const bool few = !many || g->T < (int64_t)g->B * g->max_new;
+  if (few) {
+    k->few.block_rows = rows > 16 ? 32 : 16;
+    k->few.over = 0;
+    k->few.upto = kFewRows;
+    rc = cut(g, c, false, &k->few);
+  }
+  if (many && !rc) {
+    k->many.block_rows = kTileRows;
+    k->many.over = few ? kFewRows : 0;
+    k->many.upto = 0x7fffffff;
+    rc = cut(g, c, true, &k->many);
+  }
+  return rc;
 }
 
 // Sizes alone: what the workspace goes by.
 int check_sizes(const leech_kv_cache* cache, const leech_attend_args* g, CacheShape* shape,
-                Cut* k) {
+                Cuts* k) {
   const int rc = check_cache(cache, shape);
   if (rc) return rc;
   if (!g) return set_error(LEECH_E_ARG, "the arguments are NULL");
@@ -694,7 +1048,7 @@ int check_sizes(const leech_kv_cache* cache, const leech_attend_args* g, CacheSh
     return set_error(LEECH_E_SHAPE, "a row of the page table holds fewer than 2^31 - 256 tokens");
   if (!g->q_start && g->T != g->B)
     return set_error(LEECH_E_SHAPE, "without q_start there is one new token a sequence");
-  return cut(g, *shape, k);
+  return cut_all(g, *shape, k);
 }
 
 int check_strides(const char* name, const void* p, int64_t token, int64_t head) {
@@ -706,11 +1060,53 @@ int check_strides(const char* name, const void* p, int64_t token, int64_t head) 
 }
 
 typedef void (*AttendFn)(AttendArgs);
+struct Launch {
+  AttendFn fn;
+  size_t lds;
+};
+template <int CT, int DT>
+Launch pick_dim(int block_rows) {
+  if (block_rows == 16) return {stream_kernel<CT, DT, 1>, 0};
+  if (block_rows == 32) return {stream_kernel<CT, DT, 2>, 0};
+  return {tile_kernel<CT, DT>, sizeof(TileLds<CT, DT>)};
+}
 template <int CT>
-AttendFn pick(int dim, int nt) {
-  if (dim <= 64) return nt == 1 ? stream_kernel<CT, 64, 1> : stream_kernel<CT, 64, 2>;
-  if (dim <= 128) return nt == 1 ? stream_kernel<CT, 128, 1> : stream_kernel<CT, 128, 2>;
-  return nt == 1 ? stream_kernel<CT, 256, 1> : stream_kernel<CT, 256, 2>;
+Launch pick(int dim, int block_rows) {
+  return dim <= 64    ? pick_dim<CT, 64>(block_rows)
+         : dim <= 128 ? pick_dim<CT, 128>(block_rows)
+                      : pick_dim<CT, 256>(block_rows);
+}
+
+int launch(AttendArgs a, const Cut& k, float* workspace, hipStream_t stream) {
+  a.block_rows = k.block_rows;
+  a.log_step = k.log_step;
+  a.min_steps = k.min_steps;
+  a.units = (int32_t)k.units;
+  a.split = k.split;
+  a.over = k.over;
+  a.upto = k.upto;
+  a.target = (float)k.target;
+  a.part_o = workspace;
+  a.part_ml = workspace + (int64_t)a.c.heads * k.units * k.block_rows * a.c.dim;
+  const Launch f = a.c.type == LEECH_F16    ? pick<kF16>(a.c.dim, k.block_rows)
+                   : a.c.type == LEECH_BF16 ? pick<kBf16>(a.c.dim, k.block_rows)
+                   : a.c.type == LEECH_INT8 ? pick<kInt8>(a.c.dim, k.block_rows)
+                                            : pick<kE4m3>(a.c.dim, k.block_rows);
+  hipError_t e;
+  if (f.lds > 64 * 1024) {
+    e = hipFuncSetAttribute((const void*)f.fn, hipFuncAttributeMaxDynamicSharedMemorySize,
+                            (int)f.lds);
+    if (e != hipSuccess) return hip_fail("hipFuncSetAttribute", e);
+  }
+  hipLaunchKernelGGL(f.fn, dim3((unsigned)(a.c.heads * k.units)), dim3(64 * kWaves), f.lds, stream,
+                     a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return hip_fail("attend launch", e);
+  if (!k.split) return LEECH_OK;
+  hipLaunchKernelGGL(join_kernel, dim3((unsigned)a.T, (unsigned)a.q_heads), dim3(64 * kWaves), 0,
+                     stream, a);
+  e = hipGetLastError();
+  return e == hipSuccess ? LEECH_OK : hip_fail("attend join launch", e);
 }
 
 }  // namespace
@@ -722,11 +1118,11 @@ extern "C" int leech_attend_workspace(const leech_kv_cache* cache, const leech_a
                                       size_t* bytes) {
   clear_error();
   CacheShape shape;
-  Cut k;
+  Cuts k;
   const int rc = check_sizes(cache, args, &shape, &k);
   if (rc) return rc;
   if (!bytes) return set_error(LEECH_E_ARG, "bytes is NULL");
-  *bytes = k.bytes;
+  *bytes = k.few.bytes + k.many.bytes;
   return LEECH_OK;
 }
 
@@ -734,7 +1130,7 @@ extern "C" int leech_attend(const leech_kv_cache* cache, const leech_attend_args
                             void* stream) {
   clear_error();
   AttendArgs a = {};
-  Cut k;
+  Cuts k;
   int rc = check_sizes(cache, g, &a.c, &k);
   if (rc) return rc;
   if ((g->causal != 0 && g->causal != 1) || g->window < 0)
@@ -752,7 +1148,8 @@ extern "C" int leech_attend(const leech_kv_cache* cache, const leech_attend_args
   if (((uintptr_t)g->q_start & 3) || ((uintptr_t)g->kv_len & 3) || ((uintptr_t)g->page_table & 3) ||
       ((uintptr_t)g->lse & 3))
     return set_error(LEECH_E_ARG, "misaligned device pointer");
-  if (k.bytes && (!g->workspace || g->workspace_bytes < k.bytes || ((uintptr_t)g->workspace & 15)))
+  const size_t bytes = k.few.bytes + k.many.bytes;
+  if (bytes && (!g->workspace || g->workspace_bytes < bytes || ((uintptr_t)g->workspace & 15)))
     return set_error(LEECH_E_ARG, "the workspace is NULL, misaligned or smaller than "
                                   "leech_attend_workspace says");
   a.ck = (const uint8_t*)cache->k;
@@ -781,25 +1178,10 @@ extern "C" int leech_attend(const leech_kv_cache* cache, const leech_attend_args
   a.causal = g->causal;
   a.window = g->window;
   a.scale = g->scale * kLog2e;
-  a.block_rows = k.block_rows;
-  a.log_step = k.log_step;
-  a.min_steps = k.min_steps;
-  a.units = (int32_t)k.units;
-  a.split = k.split;
-  a.target = kTarget;
-  a.part_o = (float*)g->workspace;
-  a.part_ml = a.part_o + (int64_t)a.c.heads * k.units * k.block_rows * a.c.dim;
-  AttendFn fn = cache->type == LEECH_F16    ? pick<kF16>(cache->dim, k.nt)
-                : cache->type == LEECH_BF16 ? pick<kBf16>(cache->dim, k.nt)
-                : cache->type == LEECH_INT8 ? pick<kInt8>(cache->dim, k.nt)
-                                            : pick<kE4m3>(cache->dim, k.nt);
-  hipLaunchKernelGGL(fn, dim3((unsigned)(a.c.heads * k.units)), dim3(64 * kWaves), 0,
-                     (hipStream_t)stream, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return hip_fail("attend launch", e);
-  if (!k.split) return LEECH_OK;
-  hipLaunchKernelGGL(join_kernel, dim3((unsigned)a.T, (unsigned)a.q_heads), dim3(64 * kWaves), 0,
-                     (hipStream_t)stream, a);
-  e = hipGetLastError();
-  return e == hipSuccess ? LEECH_OK : hip_fail("attend join launch", e);
+  float* room = (float*)g->workspace;
+  if (k.few.units && (rc = launch(a, k.few, room, (hipStream_t)stream))) return rc;
+  if (k.many.units &&
+      (rc = launch(a, k.many, room + k.few.bytes / sizeof(float), (hipStream_t)stream)))
+    return rc;
+  return LEECH_OK;
 }
