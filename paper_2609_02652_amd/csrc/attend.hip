@@ -12,18 +12,23 @@
 // hold.  Both operands come from memory straight into the registers that the
 // products read.
 //
-// One pass: the running maximum m and sum l of e^(s − m); when m grows, l and O
-// are scaled down.  Rows are (new token, query head of the group) of one
-// sequence and cache head, so a group's heads share every key read.
+// One pass.  A query keeps a base (of two's powers), the sum l of its weights
+// 2^(s − base) and O; the base follows the largest score seen, but only once that
+// is 2^8 above it (weights of up to 2^8 lose nothing), and l and O are scaled to
+// it.  Rows are (new token, query head of the group) of one sequence and cache
+// head, so a group's heads share every key read.
 //
 // 8-bit codes become f16, which holds all of them; a key's scale multiplies its
-// scores, a value's scale its weight, over the query's largest such scale so
-// far (weights under f16's range would lose bits).  bf16 queries over 8-bit
-// codes become f16 times a power of two a row.
+// scores, a value's its weight in the second product.  The base is then that of
+// weight times scale, log2 of the largest scale higher, so that the products'
+// f16 weights stay in range whatever the scales are; the scale of a weight in l
+// is the same, so out = O / l as before.  bf16 queries over 8-bit codes become
+// f16 times a power of two a row.
 
 #include "kv_device.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace leech {
 namespace {
@@ -46,7 +51,8 @@ struct AttendArgs {
   const int32_t *q_start, *kv_len, *table;
   int64_t T, pages;
   int32_t type, q_heads, group, B, table_pages, max_new, causal, window;
-  float scale;                // times log2 e
+  float scale;                // times log2 e, its magnitude; never 0 (2^-126 stands for it)
+  uint32_t flip;              // sign bits that a negative scale puts on the queries
   // how the work is cut (see the plan)
   int32_t block_rows, log_step, min_steps, units, split;
   int32_t over, upto;         // sequences of over < rows <= upto are this launch's
@@ -292,8 +298,17 @@ __device__ __forceinline__ float to_f16(kv_u32x4* q, float scale) {
       const uint32_t w = q[m][e];
       q[m][e] = pack2<kF16>(ldexpf(bf16_value(w & 0xFFFFu), -ex), ldexpf(bf16_value(w >> 16), -ex));
     }
-  return ldexpf(scale, ex);
+  return fmaxf(ldexpf(scale, ex), 0x1p-126f);
 }
+
+// The base that scores up to top (not yet scaled) and value scales up to big ask
+// for.  Scales under 2^-100 count as that: l then stays in range.
+template <bool CODES>
+__device__ __forceinline__ float base_for(float top, float qs, float big) {
+  if constexpr (CODES) return top * qs + __builtin_amdgcn_logf(fmaxf(big, 0x1p-100f));
+  return top * qs;
+}
+constexpr float kSlack = 8.0f;
 
 constexpr int kWaves = 4;
 
@@ -347,18 +362,18 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(AttendArgs a) {
     for (int m = 0; m < KM; ++m) {
       // the coordinates that sixteen bytes of a key hold, in their order
       const int d = H == 1 ? 32 * m + 8 * g : 64 * (m / 2) + 16 * g + 8 * (m % 2);
-      qf[t][m] = in && d < a.c.dim ? *(const kv_u32x4*)(q + d) : kv_u32x4{0, 0, 0, 0};
+      qf[t][m] = in && d < a.c.dim ? *(const kv_u32x4*)(q + d) ^ a.flip : kv_u32x4{0, 0, 0, 0};
     }
     qs[t] = a.scale;
     if (H == 2 && a.type == LEECH_BF16) qs[t] = to_f16<KM, 32>(qf[t], a.scale);
   }
 
   f32x4 o[NT][VM];
-  float m[NT], l[NT], vref[NT];
+  float base[NT], l[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    m[t] = -__builtin_inff();
-    l[t] = vref[t] = 0.0f;
+    base[t] = -__builtin_inff();
+    l[t] = 0.0f;
 #pragma unroll
     for (int v = 0; v < VM; ++v) o[t][v] = f32x4{0, 0, 0, 0};
   }
@@ -457,51 +472,54 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(AttendArgs a) {
         for (int d = 1; d < 16; d <<= 1) bad |= __shfl_xor(bad, d, 64);
         if (lost) bad = 0xFFFFu;
       }
+      float all_big = 0.0f;
+      if constexpr (H == 2) {
+#pragma unroll
+        for (int e = 0; e < R; ++e) all_big = fmaxf(all_big, vs[e]);
+        all_big = quarters_max(all_big);
+      }
       kv_u32x4 pw[NT][H];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         float x[R];
-        float top = -__builtin_inff();
 #pragma unroll
         for (int e = 0; e < R; ++e) {
-          x[e] = sc[t][e >> 2][e & 3] * qs[t];
+          x[e] = sc[t][e >> 2][e & 3];
           if constexpr (H == 2) x[e] *= ks[e];
-          if (edge) {
+        }
+        float big = all_big;
+        if (edge) {
+          big = 0.0f;
+#pragma unroll
+          for (int e = 0; e < R; ++e) {
             const int j = t0 + R * g + e;
-            x[e] = j < hi[t] && j >= lo[t]
-                       ? (bad >> e & 1 ? __builtin_nanf("") : x[e])
-                       : -__builtin_inff();
+            const bool sees = j < hi[t] && j >= lo[t];
+            x[e] = sees ? (bad >> e & 1 ? __builtin_nanf("") : x[e]) : -__builtin_inff();
+            if constexpr (H == 2) big = fmaxf(big, sees ? vs[e] : 0.0f);
           }
-          top = fmaxf(top, x[e]);
+          if constexpr (H == 2) big = quarters_max(big);
         }
-        top = fmaxf(m[t], quarters_max(top));
-        float big = 0.0f;
-        if constexpr (H == 2) {
+        float top = x[0];
 #pragma unroll
-          for (int e = 0; e < R; ++e)
-            big = fmaxf(big, edge && x[e] == -__builtin_inff() ? 0.0f : vs[e]);
-          big = fmaxf(vref[t], quarters_max(big));
-        }
-        if (__any(top > m[t] || (H == 2 && big > vref[t]))) {
-          const float base = top == -__builtin_inff() ? 0.0f : top;
-          const float f = __builtin_amdgcn_exp2f(m[t] - base);
+        for (int e = 1; e < R; ++e) top = fmaxf(top, x[e]);
+        const float want = base_for<H == 2>(quarters_max(top), qs[t], big);
+        if (__any(want > base[t] + kSlack)) {
+          // (each row by its own scores alone, whatever its neighbours do)
+          const float to = want > base[t] + kSlack ? want : base[t];
+          const float f = to > base[t] ? __builtin_amdgcn_exp2f(base[t] - to) : 1.0f;
           l[t] *= f;
-          const float fo = H == 2 ? (big > 0.0f ? f * (vref[t] / big) : 0.0f) : f;
 #pragma unroll
-          for (int v = 0; v < VM; ++v) o[t][v] *= fo;
-          m[t] = top;
-          vref[t] = big;
+          for (int v = 0; v < VM; ++v) o[t][v] *= f;
+          base[t] = to;
         }
-        const float base = m[t] == -__builtin_inff() ? 0.0f : m[t];
-        const float unit_v = H == 2 && vref[t] > 0.0f ? 1.0f / vref[t] : 0.0f;
+        const float from = base[t] == -__builtin_inff() ? 0.0f : base[t];
         float w[R];
 #pragma unroll
         for (int e = 0; e < R; ++e) {
-          const float p = __builtin_amdgcn_exp2f(x[e] - base);
-          l[t] += p;
-          w[e] = p;
-          if constexpr (H == 2)
-            w[e] = edge && x[e] == -__builtin_inff() ? 0.0f : p * (vs[e] * unit_v);
+          w[e] = __builtin_amdgcn_exp2f(fmaf(x[e], qs[t], -from));
+          l[t] += w[e];
+          // (what a row does not see may have any scale)
+          if constexpr (H == 2) w[e] = x[e] == -__builtin_inff() ? 0.0f : w[e] * vs[e];
         }
 #pragma unroll
         for (int i = 0; i < H; ++i)
@@ -530,12 +548,12 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(AttendArgs a) {
     }
   }
 
-  // the waves join: each scales its part to the largest maximum of a row
+  // the waves join: each scales its part to the largest base of a row
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     l[t] = quarters_sum(l[t]);
     if (g == 0) {
-      stats[wave][16 * t + col][0] = m[t];
+      stats[wave][16 * t + col][0] = base[t];
       stats[wave][16 * t + col][1] = l[t];
     }
   }
@@ -546,8 +564,7 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(AttendArgs a) {
     float top = -__builtin_inff();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stats[w][16 * t + col][0]);
-    f[t] = __builtin_amdgcn_exp2f(m[t] - (top == -__builtin_inff() ? 0.0f : top));
-    if (H == 2) f[t] *= vref[t];
+    f[t] = __builtin_amdgcn_exp2f(base[t] - (top == -__builtin_inff() ? 0.0f : top));
   }
   const bool whole = s.parts == 1;
   const int64_t part_row = ((int64_t)h * a.units + unit) * a.block_rows;
@@ -614,16 +631,17 @@ template <int DT>
 constexpr int kTileTokens = DT > 128 ? 32 : 64;
 
 // LDS of the tile kernel: two buffers of keys and values (as the products take
-// them, two bytes an element), of their scales, then for three tiles which
-// tokens' values are not finite, and for four where their tokens lie.
+// them, two bytes an element), of their scales and the largest value scale; for
+// three tiles which tokens have no number for a value, or no page; for four where
+// the tokens lie.
 template <int CT, int DT>
 struct TileLds {
   static constexpr int TOK = kTileTokens<DT>;
   kv_u32x4 k[2][TOK * DT / 8];
   kv_u32x4 v[2][TOK * DT / 8];
-  float ks[2][TOK], vs[2][TOK];
+  float ks[2][TOK], vs[2][TOK], big[2];
   uint32_t bad[3][TOK / 8];
-  int64_t where[4][TOK / 16];       // slot of each sixteen tokens, -1: no such page
+  int64_t where[4][TOK / 16];       // slot of each sixteen tokens
 };
 
 // A workgroup is a unit of up to 128 rows, a wave 32 of them; all share the keys
@@ -686,7 +704,7 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
 #pragma unroll
   for (int m = 0; m < KM; ++m) {
     const int d = 16 * m + 8 * half;
-    qf[m] = in && d < a.c.dim ? *(const kv_u32x4*)(q + d) : kv_u32x4{0, 0, 0, 0};
+    qf[m] = in && d < a.c.dim ? *(const kv_u32x4*)(q + d) ^ a.flip : kv_u32x4{0, 0, 0, 0};
   }
   float qs = a.scale;
   if (CODES && a.type == LEECH_BF16) qs = to_f16<KM, 64>(qf, a.scale);
@@ -696,40 +714,45 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
   for (int v = 0; v < VM; ++v)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[v][e] = 0.0f;
-  float m = -__builtin_inff(), l = 0.0f, vref = 0.0f;
+  float base = -__builtin_inff(), l = 0.0f;
 
   const int row_bytes = a.c.dim * S;
   const int32_t* table = a.table + b * a.table_stride;
   const int first16 = lo_first & ~15, last16 = (hi_last - 1) & ~15;
-  const auto slot16 = [&](int step, int i) {       // of sixteen tokens, clamped to those seen
-    int j = step * TOK + 16 * i;
+  // Where sixteen tokens lie (clamped to those that are seen), by the thread of
+  // each eight of a tile; those of no page count as without numbers.
+  int64_t slot = 0;
+  uint32_t lost = 0;
+  const auto look_up = [&](int step) {
+    int j = step * TOK + 16 * (tid >> 1);
     j = j < first16 ? first16 : j > last16 ? last16 : j;
     const int p = table[j >> a.c.log_page];
-    return p < 0 || p >= a.pages ? (int64_t)-1
-                                 : (((int64_t)p * a.c.heads + h) << a.c.log_page) +
-                                       (j & ((1 << a.c.log_page) - 1));
+    lost = p < 0 || p >= a.pages ? 0xFFu : 0u;
+    slot = (((int64_t)(lost ? 0 : p) * a.c.heads + h) << a.c.log_page) +
+           (j & ((1 << a.c.log_page) - 1));
+  };
+  const auto note = [&](int step) {
+    lds.bad[step % 3][tid] = lost;
+    if (!(tid & 1)) lds.where[step & 3][tid >> 1] = slot;
   };
   kv_u32x4 kw[NL], vw[NL];
   float sc = 0.0f;
+  // Columns past the head's dimension read others again: those of the queries are 0,
+  // those of out are not kept.
   const auto load = [&](int step) {
     const int64_t* where = lds.where[step & 3];
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int at = i * 64 * kWaves + tid, t = at / LC, c = at % LC;
-      const int64_t w = where[t >> 4];
-      kw[i] = w >= 0 && 16 * c < row_bytes
-                  ? *(const kv_u32x4*)(a.ck + (w + (t & 15)) * row_bytes + 16 * c)
-                  : kv_u32x4{0, 0, 0, 0};
+      kw[i] = *(const kv_u32x4*)(a.ck + (where[t >> 4] + (t & 15)) * row_bytes +
+                                 (16 * c < row_bytes ? 16 * c : 0));
       const int run = at / DT, d = at % DT;
-      const int64_t x = where[run * R >> 4];
-      vw[i] = x >= 0 && d < a.c.dim
-                  ? *(const kv_u32x4*)(a.cv + (x + (run * R & 15)) * row_bytes + 16 * d)
-                  : kv_u32x4{0, 0, 0, 0};
+      vw[i] = *(const kv_u32x4*)(a.cv + (where[run * R >> 4] + (run * R & 15)) * row_bytes +
+                                 16 * (d < a.c.dim ? d : 0));
     }
     if constexpr (CODES) {
       const int t = tid & (TOK - 1);
-      const int64_t w = where[t >> 4];
-      if (tid < 2 * TOK && w >= 0) sc = (tid < TOK ? a.sk : a.sv)[w + (t & 15)];
+      sc = ((tid & TOK) ? a.sv : a.sk)[where[t >> 4] + (t & 15)];
     }
   };
   const auto keep = [&](int step) {
@@ -747,32 +770,36 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
       }
       // values behind some row's mask must be numbers; a token that has none
       // counts as NaN for the rows that see it
-      const bool lost = lds.where[step & 3][run * R >> 4] < 0;
-      uint32_t bad = 0;
-      if (edge) bad = drop_non_finite<CT>(vw[i]);
-      if (lost) bad = 0xFFFFu;
+      if (CT != kInt8 && edge) {
+        const uint32_t bad = drop_non_finite<CT>(vw[i]);
+        if (bad) {
+          atomicOr(&lds.bad[step % 3][run * R / 8], bad & 0xFFu);
+          if (CODES) atomicOr(&lds.bad[step % 3][run * R / 8 + 1], bad >> 8);
+        }
+      }
       if constexpr (CODES) {
         lds.v[buf][2 * run * DT + d] = operand<CT>(vw[i], 0);
         lds.v[buf][(2 * run + 1) * DT + d] = operand<CT>(vw[i], 1);
-        if (bad) {
-          atomicOr(&lds.bad[step % 3][2 * run], bad & 0xFFu);
-          atomicOr(&lds.bad[step % 3][2 * run + 1], bad >> 8);
-        }
       } else {
         lds.v[buf][run * DT + d] = vw[i];
-        if (bad) atomicOr(&lds.bad[step % 3][run], bad & 0xFFu);
       }
     }
-    if constexpr (CODES)
+    if constexpr (CODES) {
       if (tid < 2 * TOK) (tid < TOK ? lds.ks : lds.vs)[buf][tid & (TOK - 1)] = sc;
+      float big = sc;                   // every TOK threads hold a whole tile's scales
+#pragma unroll
+      for (int x = 1; x < TOK; x <<= 1) big = fmaxf(big, __shfl_xor(big, x, 64));
+      if (tid == TOK) lds.big[buf] = big;
+    }
   };
 
   if (step0 < step1) {
-    if (tid < TOK / 16) {
-      lds.where[step0 & 3][tid] = slot16(step0, tid);
-      lds.where[(step0 + 1) & 3][tid] = slot16(step0 + 1, tid);
+    if (tid < TOK / 8) {
+      look_up(step0);
+      note(step0);
+      look_up(step0 + 1);
+      note(step0 + 1);
     }
-    if (tid < TOK / 8) lds.bad[0][tid] = lds.bad[1][tid] = lds.bad[2][tid] = 0;
     __syncthreads();
     load(step0);
     keep(step0);
@@ -781,83 +808,89 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
   for (int step = step0; step < step1; ++step) {
     const int buf = step & 1, t0 = step * TOK;
     const bool more = step + 1 < step1;
-    int64_t ahead = 0;
     if (more) {
       load(step + 1);
-      if (tid < TOK / 16) ahead = slot16(step + 2, tid);
-      if (tid < TOK / 8) lds.bad[(step + 2) % 3][tid] = 0;
+      if (tid < TOK / 8) look_up(step + 2);
     }
     if (live && t0 < whi && t0 + TOK > wlo) {
-      f32x16 sc32[NK];
+      f32x16 x[NK];
 #pragma unroll
       for (int n = 0; n < NK; ++n) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sc32[n][e] = 0.0f;
+        for (int e = 0; e < 16; ++e) x[n][e] = 0.0f;
         const int t = 32 * n + 16 * (col >> 4) + 8 * (col >> 2 & 1) + 4 * (col >> 3 & 1) + (col & 3);
 #pragma unroll
         for (int k = 0; k < KM; ++k)
-          sc32[n] = mfma32<CT>(lds.k[buf][t * CH + (2 * k + half ^ (t & SWZ))], qf[k], sc32[n]);
+          x[n] = mfma32<CT>(lds.k[buf][t * CH + (2 * k + half ^ (t & SWZ))], qf[k], x[n]);
       }
       // score e of tile n: token 32 n + 16 (e / 8) + 8 half + e % 8
+      if constexpr (CODES)
+#pragma unroll
+        for (int n = 0; n < 4 * NK; ++n) {
+          const f32x4 y = *(const f32x4*)&lds.ks[buf][16 * (n >> 1) + 8 * half + 4 * (n & 1)];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[n >> 2][4 * (n & 3) + e] *= y[e];
+        }
       uint32_t bad = 0;
 #pragma unroll
       for (int n = 0; n < 2 * NK; ++n) bad |= lds.bad[step % 3][2 * n + half] << (8 * n);
       const bool edge = t0 + TOK > whi_first || t0 < wlo_last || __any(bad != 0);
-      float top = -__builtin_inff(), big = 0.0f;
+      float big = CODES ? lds.big[buf] : 0.0f;
+      if (edge) {
+        big = 0.0f;
+#pragma unroll
+        for (int n = 0; n < 4 * NK; ++n) {
+          const int j0 = 16 * (n >> 1) + 8 * half + 4 * (n & 1);
+          f32x4 y = {0, 0, 0, 0};
+          if constexpr (CODES) y = *(const f32x4*)&lds.vs[buf][j0];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int j = t0 + j0 + e;
+            const bool sees = j < hi && j >= lo;
+            const float z = bad >> (4 * n + e) & 1 ? __builtin_nanf("") : x[n >> 2][4 * (n & 3) + e];
+            x[n >> 2][4 * (n & 3) + e] = sees ? z : -__builtin_inff();
+            if constexpr (CODES) big = fmaxf(big, sees ? y[e] : 0.0f);
+          }
+        }
+        if constexpr (CODES) {
+          const Pair p = swapped<64>(big);
+          big = fmaxf(p.a, p.b);
+        }
+      }
+      float top = x[0][0];
 #pragma unroll
       for (int n = 0; n < NK; ++n)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float x = sc32[n][e] * qs;
-          const int j = 32 * n + 16 * (e >> 3) + 8 * half + (e & 7);
-          if constexpr (CODES) x *= lds.ks[buf][j];
-          if (edge) {
-            const bool sees = t0 + j < hi && t0 + j >= lo;
-            x = sees ? (bad >> (16 * n + e) & 1 ? __builtin_nanf("") : x) : -__builtin_inff();
-            if constexpr (CODES)
-              if (sees) big = fmaxf(big, lds.vs[buf][j]);
-          } else if constexpr (CODES) {
-            big = fmaxf(big, lds.vs[buf][j]);
-          }
-          sc32[n][e] = x;
-          top = fmaxf(top, x);
-        }
-      Pair p = swapped<64>(top);
-      top = fmaxf(m, fmaxf(p.a, p.b));
-      if constexpr (CODES) {
-        p = swapped<64>(big);
-        big = fmaxf(vref, fmaxf(p.a, p.b));
-      }
-      if (__any(top > m || (CODES && big > vref))) {
-        const float f = __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.0f : top));
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, x[n][e]);
+      const Pair p = swapped<64>(top);
+      const float want = base_for<CODES>(fmaxf(p.a, p.b), qs, big);
+      if (__any(want > base + kSlack)) {
+        // (each row by its own scores alone, whatever its neighbours do)
+        const float to = want > base + kSlack ? want : base;
+        const float f = to > base ? __builtin_amdgcn_exp2f(base - to) : 1.0f;
         l *= f;
-        const float fo = CODES ? (big > 0.0f ? f * (vref / big) : 0.0f) : f;
 #pragma unroll
-        for (int v = 0; v < VM; ++v) o[v] *= fo;
-        m = top;
-        vref = big;
+        for (int v = 0; v < VM; ++v) o[v] *= f;
+        base = to;
       }
-      const float base = m == -__builtin_inff() ? 0.0f : m;
-      const float unit_v = CODES && vref > 0.0f ? 1.0f / vref : 0.0f;
+      const float from = base == -__builtin_inff() ? 0.0f : base;
       kv_u32x4 pw[2 * NK];
 #pragma unroll
-      for (int n = 0; n < NK; ++n)
+      for (int n = 0; n < 4 * NK; ++n) {
+        f32x4 y = {1, 1, 1, 1};
+        if constexpr (CODES) y = *(const f32x4*)&lds.vs[buf][16 * (n >> 1) + 8 * half + 4 * (n & 1)];
+        float w[4];
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-          float w[2];
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const float x = sc32[n][e + y];
-            const float pe = __builtin_amdgcn_exp2f(x - base);
-            l += pe;
-            w[y] = pe;
-            if constexpr (CODES) {
-              const int j = 32 * n + 16 * (e >> 3) + 8 * half + (e & 7) + y;
-              w[y] = edge && x == -__builtin_inff() ? 0.0f : pe * (lds.vs[buf][j] * unit_v);
-            }
-          }
-          pw[2 * n + (e >> 3)][(e & 7) >> 1] = pack2<CT>(w[0], w[1]);
+        for (int e = 0; e < 4; ++e) {
+          const float z = x[n >> 2][4 * (n & 3) + e];
+          w[e] = __builtin_amdgcn_exp2f(fmaf(z, qs, -from));
+          l += w[e];
+          // (what a row does not see may have any scale)
+          if constexpr (CODES) w[e] = z == -__builtin_inff() ? 0.0f : w[e] * y[e];
         }
+        pw[n >> 1][2 * (n & 1)] = pack2<CT>(w[0], w[1]);
+        pw[n >> 1][2 * (n & 1) + 1] = pack2<CT>(w[2], w[3]);
+      }
 #pragma unroll
       for (int n = 0; n < 2 * NK; ++n)
 #pragma unroll
@@ -866,7 +899,7 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
     }
     if (more) {
       keep(step + 1);
-      if (tid < TOK / 16) lds.where[(step + 2) & 3][tid] = ahead;
+      if (tid < TOK / 8) note(step + 2);
     }
     __syncthreads();
   }
@@ -874,7 +907,6 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
   Pair p = swapped<64>(l);
   l = p.a + p.b;
   if (!in) return;
-  const float fv = CODES ? vref : 1.0f;
   if (s.parts > 1) {
     const int64_t at = ((int64_t)h * a.units + u0 + tile * s.parts + part) * kTileRows + wrow + col;
 #pragma unroll
@@ -884,15 +916,15 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
         const int d = 32 * v + 8 * i + 4 * half;
         if (d < a.c.dim)
           *(f32x4*)(a.part_o + at * a.c.dim + d) =
-              f32x4{o[v][4 * i], o[v][4 * i + 1], o[v][4 * i + 2], o[v][4 * i + 3]} * fv;
+              f32x4{o[v][4 * i], o[v][4 * i + 1], o[v][4 * i + 2], o[v][4 * i + 3]};
       }
     if (half == 0) {
-      a.part_ml[2 * at] = m;
+      a.part_ml[2 * at] = base;
       a.part_ml[2 * at + 1] = l;
     }
     return;
   }
-  const float inv = (l != 0.0f ? 1.0f / l : 0.0f) * fv;
+  const float inv = l != 0.0f ? 1.0f / l : 0.0f;          // a NaN sum stays one
   const int64_t t = s.first + r / a.group;
   const int qh = h * a.group + r % a.group;
   uint16_t* out = a.out + t * a.o_token + qh * a.o_head;
@@ -910,7 +942,7 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
                                   : kv_u32x2{pack2<kBf16>(x[0], x[1]), pack2<kBf16>(x[2], x[3])};
     }
   if (a.lse && half == 0)
-    a.lse[t * a.q_heads + qh] = l != 0.0f ? (m + log2f(l)) * kLn2 : -__builtin_inff();
+    a.lse[t * a.q_heads + qh] = l != 0.0f ? (base + log2f(l)) * kLn2 : -__builtin_inff();
 }
 
 // Joins the parts of one row (a token's query head), a wave a quarter of them.
@@ -1177,7 +1209,8 @@ extern "C" int leech_attend(const leech_kv_cache* cache, const leech_attend_args
   a.max_new = g->max_new;
   a.causal = g->causal;
   a.window = g->window;
-  a.scale = g->scale * kLog2e;
+  a.scale = std::max(std::fabs(g->scale) * kLog2e, 0x1p-126f);
+  a.flip = g->scale < 0.0f ? 0x80008000u : 0u;
   float* room = (float*)g->workspace;
   if (k.few.units && (rc = launch(a, k.few, room, (hipStream_t)stream))) return rc;
   if (k.many.units &&
