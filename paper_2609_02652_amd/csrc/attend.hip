@@ -56,6 +56,7 @@ struct AttendArgs {
   // how the work is cut (see the plan)
   int32_t block_rows, log_step, min_steps, units, split;
   int32_t over, upto;         // sequences of over < rows <= upto are this launch's
+  int32_t slices;             // workgroups that join a tile's rows
   float target;
   float *part_o, *part_ml;    // [head][unit][row][dim], [head][unit][row][2]
 };
@@ -70,6 +71,7 @@ struct AttendArgs {
 struct Sequence {
   int64_t first;              // row of q of its first new token
   int32_t n, rows, tiles, len, steps, parts;
+  int32_t at;                 // what was looked for, counted from the sequence's first
 };
 
 __device__ __forceinline__ int64_t start_of(const AttendArgs& a, int b) {
@@ -78,7 +80,7 @@ __device__ __forceinline__ int64_t start_of(const AttendArgs& a, int b) {
 }
 
 __device__ __forceinline__ Sequence sequence(const AttendArgs& a, int b) {
-  Sequence s = {0, 0, 0, 0, 0, 0, 1};
+  Sequence s = {0, 0, 0, 0, 0, 0, 1, 0};
   if (b >= a.B) return s;
   s.first = start_of(a, b);
   const int64_t n = start_of(a, b + 1) - s.first;
@@ -96,20 +98,37 @@ __device__ __forceinline__ Sequence sequence(const AttendArgs& a, int b) {
   return s;
 }
 
-__device__ __forceinline__ int wave_scan(int v) {       // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(v, d, 64);
-    if (lane >= d) v += o;
-  }
+// A lane's value from the lane that a data-parallel-primitive control names; rows
+// and banks without one keep `old`.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved(int old, int v) {
+  return __builtin_amdgcn_update_dpp(old, v, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int wave_scan(int v) {       // inclusive sums
+  v += moved<0x111, 0xF>(0, v);                         // row_shr 1, 2, 4, 8
+  v += moved<0x112, 0xF>(0, v);
+  v += moved<0x114, 0xF>(0, v);
+  v += moved<0x118, 0xF>(0, v);
+  v += moved<0x142, 0xA>(0, v);                         // row 0's last to row 1, row 2's to row 3
+  v += moved<0x143, 0xC>(0, v);                         // lane 31 to rows 2 and 3
   return v;
 }
+__device__ __forceinline__ float wave_total(float v) {
+  const auto add = [](float a, int b) { return a + __builtin_bit_cast(float, b); };
+  v = add(v, moved<0x111, 0xF>(0, __builtin_bit_cast(int, v)));
+  v = add(v, moved<0x112, 0xF>(0, __builtin_bit_cast(int, v)));
+  v = add(v, moved<0x114, 0xF>(0, __builtin_bit_cast(int, v)));
+  v = add(v, moved<0x118, 0xF>(0, __builtin_bit_cast(int, v)));
+  v = add(v, moved<0x142, 0xA>(0, __builtin_bit_cast(int, v)));
+  v = add(v, moved<0x143, 0xC>(0, __builtin_bit_cast(int, v)));
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
 
-// The sequence, and the number of its first unit, of unit `unit` (by_unit) or of
-// row `token` of q; false if there is none.
-__device__ __forceinline__ bool find(const AttendArgs& a, bool by_unit, int unit, int64_t token,
-                                     Sequence* out, int* seq, int* first_unit) {
+// The sequence, and the number of its first unit, of a unit or of a tile (numbered
+// alike, parts left out); false if there is none.
+enum Number { kUnitNumber, kTileNumber };
+__device__ __forceinline__ bool find(const AttendArgs& a, Number what, int number, Sequence* out,
+                                     int* seq, int* first_unit) {
   const int lane = threadIdx.x & 63;
   const Sequence head = sequence(a, lane);
   int steps = 0x7fffffff;                               // of a part
@@ -117,23 +136,19 @@ __device__ __forceinline__ bool find(const AttendArgs& a, bool by_unit, int unit
     float total = 0.0f;
     for (int b = 0; b < a.B; b += 64) {
       const Sequence s = b ? sequence(a, b + lane) : head;
-      float w = (float)s.tiles * (float)s.steps;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) w += __shfl_xor(w, d, 64);
-      total += w;
+      total += wave_total((float)s.tiles * (float)s.steps);
     }
     const float share = ceilf(total * (float)a.c.heads / a.target);
     steps = share > 1e9f ? 1000000000 : share > (float)a.min_steps ? (int)share : a.min_steps;
   }
-  int before = 0;
+  int before = 0, units_before = 0;
   for (int b = 0; b < a.B; b += 64) {
     Sequence s = b ? sequence(a, b + lane) : head;
     s.parts = a.split ? (s.steps + steps - 1) / steps : 1;
-    const int own = s.tiles * s.parts, upto = before + wave_scan(own);
-    const bool hit = by_unit ? unit >= upto - own && unit < upto
-                             : s.tiles && token >= s.first &&
-                                   token - s.first < (s.n < a.max_new ? s.n : a.max_new);
-    const uint64_t mask = __ballot(hit);
+    const int units = s.tiles * s.parts, own = what == kUnitNumber ? units : s.tiles;
+    const int upto = before + wave_scan(own);
+    const uint64_t mask = __ballot(number >= upto - own && number < upto);
+    const int units_upto = what == kUnitNumber ? upto : units_before + wave_scan(units);
     if (mask) {
       const int at = __ffsll((unsigned long long)mask) - 1;
       out->first = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)s.first, at);
@@ -143,11 +158,13 @@ __device__ __forceinline__ bool find(const AttendArgs& a, bool by_unit, int unit
       out->len = __builtin_amdgcn_readlane(s.len, at);
       out->steps = __builtin_amdgcn_readlane(s.steps, at);
       out->parts = __builtin_amdgcn_readlane(s.parts, at);
+      out->at = number - __builtin_amdgcn_readlane(upto - own, at);
       *seq = b + at;
-      *first_unit = __builtin_amdgcn_readlane(upto - own, at);
+      *first_unit = __builtin_amdgcn_readlane(units_upto - units, at);
       return true;
     }
     before = __builtin_amdgcn_readlane(upto, 63);
+    units_before = __builtin_amdgcn_readlane(units_upto, 63);
   }
   return false;
 }
@@ -318,7 +335,7 @@ constexpr int kWaves = 4;
 // are 32 registers a lane each at DT = 128, the next step's keys loading while
 // this one's weights and values are worked on and the other way round.
 template <int CT, int DT, int NT>
-__global__ __launch_bounds__(64 * kWaves) void stream_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void stream_kernel(AttendArgs a) {
   constexpr int R = kRun<CT>, TOK = kStep<CT>, NU = R / 4;
   constexpr int KC = DT * kBytes<CT> / 64;       // sixteen-byte loads of a key row's lane
   constexpr int KM = DT / 32;                    // products along a head
@@ -331,8 +348,8 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(AttendArgs a) {
   const int h = blockIdx.x % a.c.heads, unit = blockIdx.x / a.c.heads;
   Sequence s;
   int b, u0;
-  if (!find(a, true, unit, 0, &s, &b, &u0)) return;
-  const int tile = (unit - u0) / s.parts, part = (unit - u0) % s.parts;
+  if (!find(a, kUnitNumber, unit, &s, &b, &u0)) return;
+  const int tile = s.at / s.parts, part = s.at % s.parts;
   const int row0 = tile * a.block_rows;
   const int rows = s.rows - row0 < 16 * NT ? s.rows - row0 : 16 * NT;
   const int col = lane & 15, g = lane >> 4;
@@ -637,7 +654,7 @@ constexpr int kTileTokens = DT > 128 ? 32 : 64;
 template <int CT, int DT>
 struct TileLds {
   static constexpr int TOK = kTileTokens<DT>;
-  kv_u32x4 k[2][TOK * DT / 8];
+  kv_u32x4 k[2][TOK * (DT / 8 + 1)];
   kv_u32x4 v[2][TOK * DT / 8];
   float ks[2][TOK], vs[2][TOK], big[2];
   uint32_t bad[3][TOK / 8];
@@ -651,16 +668,15 @@ struct TileLds {
 // transposed as in stream_kernel: row m of a 32-token key tile is token 16·(m / 16)
 // + 8·(m / 4 % 2) + 4·(m / 8 % 2) + m % 4, so that a lane's scores are of whole
 // runs of eight tokens, those whose values it multiplies next.  Keys lie in LDS
-// row by row, chunk c of row r in place c ^ r % 16 (as far as a row has places),
-// which puts the chunks that a read takes at once in different banks.
+// row by row with sixteen bytes between, which puts the chunks of eight rows that a
+// read takes at once in different banks.
 template <int CT, int DT>
 __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(AttendArgs a) {
   constexpr int TOK = kTileTokens<DT>, S = kBytes<CT>, R = kRun<CT>;
   constexpr int NK = TOK / 32;                 // key tiles of 32
   constexpr int KM = DT / 16;                  // products along a head
   constexpr int VM = DT / 32;                  // tiles of coordinates
-  constexpr int CH = DT / 8;                   // LDS chunks of a key row
-  constexpr int SWZ = CH < 16 ? CH - 1 : 15;
+  constexpr int CH = DT / 8 + 1;               // LDS chunks of a key row, one of them empty
   constexpr int LC = DT * S / 16;              // sixteen-byte loads of a key row
   constexpr int NL = TOK * LC / (64 * kWaves); // of a thread, for keys; as many for values
   constexpr bool CODES = S == 1;
@@ -670,11 +686,11 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
   const int h = blockIdx.x % a.c.heads, unit = blockIdx.x / a.c.heads;
   Sequence s;
   int b, u0;
-  if (!find(a, true, unit, 0, &s, &b, &u0)) return;
+  if (!find(a, kUnitNumber, unit, &s, &b, &u0)) return;
   // (starts that do not ascend can number units that the workspace does not hold)
   if (s.parts > 1 && u0 + s.tiles * s.parts > a.units) return;
   // the tiles that see most keys first: they run longest
-  const int tile = s.tiles - 1 - (unit - u0) / s.parts, part = (unit - u0) % s.parts;
+  const int tile = s.tiles - 1 - s.at / s.parts, part = s.at % s.parts;
   const int row0 = tile * kTileRows;
   const int rows = s.rows - row0 < kTileRows ? s.rows - row0 : kTileRows;
   const int col = lane & 31, half = lane >> 5;
@@ -763,10 +779,10 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
       const int at = i * 64 * kWaves + tid, t = at / LC, c = at % LC;
       const int run = at / DT, d = at % DT;
       if constexpr (CODES) {
-        lds.k[buf][t * CH + (2 * c ^ (t & SWZ))] = operand<CT>(kw[i], 0);
-        lds.k[buf][t * CH + (2 * c + 1 ^ (t & SWZ))] = operand<CT>(kw[i], 1);
+        lds.k[buf][t * CH + 2 * c] = operand<CT>(kw[i], 0);
+        lds.k[buf][t * CH + 2 * c + 1] = operand<CT>(kw[i], 1);
       } else {
-        lds.k[buf][t * CH + (c ^ (t & SWZ))] = kw[i];
+        lds.k[buf][t * CH + c] = kw[i];
       }
       // values behind some row's mask must be numbers; a token that has none
       // counts as NaN for the rows that see it
@@ -821,8 +837,16 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
         const int t = 32 * n + 16 * (col >> 4) + 8 * (col >> 2 & 1) + 4 * (col >> 3 & 1) + (col & 3);
 #pragma unroll
         for (int k = 0; k < KM; ++k)
-          x[n] = mfma32<CT>(lds.k[buf][t * CH + (2 * k + half ^ (t & SWZ))], qf[k], x[n]);
+          x[n] = mfma32<CT>(lds.k[buf][t * CH + 2 * k + half], qf[k], x[n]);
       }
+      // key reads run six ahead of the products: two waves a SIMD do not hide them all
+      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+      for (int i = 0; i < NK * KM - 6; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
       // score e of tile n: token 32 n + 16 (e / 8) + 8 half + e % 8
       if constexpr (CODES)
 #pragma unroll
@@ -945,62 +969,67 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
     a.lse[t * a.q_heads + qh] = l != 0.0f ? (base + log2f(l)) * kLn2 : -__builtin_inff();
 }
 
-// Joins the parts of one row (a token's query head), a wave a quarter of them.
+// Joins the parts of a unit's rows: a workgroup is a tile of one sequence and cache
+// head, a wave a row at a time.  A row's parts are weighed first, a lane a part,
+// then summed, a lane four coordinates, with no load waiting for another.
 __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a) {
-  __shared__ float acc[kWaves][kMaxHeadDim];
-  __shared__ float stats[kWaves][2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t t = blockIdx.x;
-  const int qh = blockIdx.y, h = qh / a.group;
+  const int h = blockIdx.x % a.c.heads;
+  const int slice = blockIdx.x / a.c.heads % a.slices, at_tile = blockIdx.x / a.c.heads / a.slices;
   Sequence s;
   int b, u0;
-  if (!find(a, false, 0, t, &s, &b, &u0) || s.parts == 1) return;
-  const int row = (int)(t - s.first) * a.group + qh % a.group;
-  // (starts that do not ascend can number units that the launch did not hold)
-  if (u0 + (row / a.block_rows + 1) * s.parts > a.units) return;
-  const int64_t first = ((int64_t)h * a.units + u0 + row / a.block_rows * s.parts) * a.block_rows +
-                        row % a.block_rows;
-  float top = -__builtin_inff(), sum = 0.0f;
-  f32x4 x = {0, 0, 0, 0};
-  for (int p = wave; p < s.parts; p += kWaves) {
-    const int64_t at = first + (int64_t)p * a.block_rows;
-    const float pm = a.part_ml[2 * at], pl = a.part_ml[2 * at + 1];
-    f32x4 y = {0, 0, 0, 0};
-    if (4 * lane < a.c.dim) y = *(const f32x4*)(a.part_o + at * a.c.dim + 4 * lane);
-    const float most = fmaxf(top, pm), base = most == -__builtin_inff() ? 0.0f : most;
-    const float f0 = __builtin_amdgcn_exp2f(top - base), f1 = __builtin_amdgcn_exp2f(pm - base);
-    sum = sum * f0 + pl * f1;
-    x = x * f0 + y * f1;
-    top = most;
-  }
-  if (lane == 0) {
-    stats[wave][0] = top;
-    stats[wave][1] = sum;
-  }
-  if (4 * lane < a.c.dim) *(f32x4*)&acc[wave][4 * lane] = x;
-  __syncthreads();
-  float most = -__builtin_inff(), total = 0.0f;
+  if (!find(a, kTileNumber, at_tile, &s, &b, &u0) || s.parts == 1) return;
+  const int tile = s.at;
+  // (starts that do not ascend can number units that the workspace does not hold)
+  if (u0 + s.tiles * s.parts > a.units) return;
+  const int row0 = tile * a.block_rows;
+  const int rows = s.rows - row0 < a.block_rows ? s.rows - row0 : a.block_rows;
+  const int64_t first = ((int64_t)h * a.units + u0 + tile * s.parts) * a.block_rows;
+  const int lanes = a.c.dim / 4;                       // of a part's row
+  const int each = lanes <= 16 ? 4 : lanes <= 32 ? 2 : 1;   // parts that a wave reads at once
+  const int sub = lane / (64 / each), c = 4 * (lane % (64 / each));
+  const bool in = c < a.c.dim;
+  for (int r = slice * kWaves + wave; r < rows; r += kWaves * a.slices) {
+    const int64_t at = first + r;
+    float top = -__builtin_inff();
+    for (int p = lane; p < s.parts; p += 64)
+      top = fmaxf(top, a.part_ml[2 * (at + (int64_t)p * a.block_rows)]);
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) most = fmaxf(most, stats[w][0]);
-  const float base = most == -__builtin_inff() ? 0.0f : most;
-  float f[kWaves];
+    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    const float base = top == -__builtin_inff() ? 0.0f : top;
+    float sum = 0.0f;
+    f32x4 x = {0, 0, 0, 0};
+    for (int p0 = 0; p0 < s.parts; p0 += 64) {
+      float f = 0.0f;
+      if (p0 + lane < s.parts) {
+        const kv_f32x2 y = *(const kv_f32x2*)(a.part_ml + 2 * (at + (int64_t)(p0 + lane) * a.block_rows));
+        f = __builtin_amdgcn_exp2f(y[0] - base);
+        sum += f * y[1];
+      }
+      const int n = s.parts - p0 < 64 ? s.parts - p0 : 64;
+#pragma unroll 8
+      for (int p = 0; p < n; p += each) {
+        const float w = __shfl(f, p + sub, 64);
+        if (in && p + sub < n)
+          x += *(const f32x4*)(a.part_o + (at + (int64_t)(p0 + p + sub) * a.block_rows) * a.c.dim + c) * w;
+      }
+    }
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    f[w] = __builtin_amdgcn_exp2f(stats[w][0] - base);
-    total += stats[w][1] * f[w];
-  }
-  const float inv = total != 0.0f ? 1.0f / total : 0.0f;
-  const int d = threadIdx.x;
-  if (d < a.c.dim) {
-    float y = 0.0f;
+    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
+    for (int d = 64 / each; d < 64; d <<= 1)
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) y += acc[w][d] * f[w];
-    y *= inv;
-    a.out[t * a.o_token + qh * a.o_head + d] =
-        (uint16_t)(a.type == LEECH_F16 ? half_bits(y) : bf16_bits(y));
+      for (int e = 0; e < 4; ++e) x[e] += __shfl_xor(x[e], d, 64);
+    const int64_t t = s.first + (row0 + r) / a.group;
+    const int qh = h * a.group + (row0 + r) % a.group;
+    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;       // a NaN sum stays one
+    x *= inv;
+    if (in && sub == 0)
+      *(kv_u32x2*)(a.out + t * a.o_token + qh * a.o_head + c) =
+          a.type == LEECH_F16 ? kv_u32x2{pack2<kF16>(x[0], x[1]), pack2<kF16>(x[2], x[3])}
+                              : kv_u32x2{pack2<kBf16>(x[0], x[1]), pack2<kBf16>(x[2], x[3])};
+    if (a.lse && lane == 0)
+      a.lse[t * a.q_heads + qh] = sum != 0.0f ? (top + log2f(sum)) * kLn2 : -__builtin_inff();
   }
-  if (a.lse && d == 0)
-    a.lse[t * a.q_heads + qh] = total != 0.0f ? (most + log2f(total)) * kLn2 : -__builtin_inff();
 }
 
 // ------------------------------------------------------------------ host side
@@ -1012,7 +1041,7 @@ constexpr int kMinTokens = 256;        // keys of a part, at least
 // One launch's share of a call: a function of sizes alone.
 struct Cut {
   int block_rows, log_step, min_steps, split, over, upto, target;
-  int64_t units;
+  int64_t tiles, units;
   size_t bytes;
 };
 struct Cuts {
@@ -1028,34 +1057,36 @@ int cut(const leech_attend_args* g, const CacheShape& c, bool many, Cut* k) {
   const int64_t least = (T + k->block_rows - 1) / k->block_rows;
   k->split = keys > kMinTokens && least * c.heads < k->target;
   // (two more for the roundings of the plan's f32 total)
-  k->units = T / k->block_rows + std::min<int64_t>(g->B, g->T) +
-             (k->split ? (k->target + c.heads - 1) / c.heads + 2 : 0);
-  if (k->units * c.heads * 64 * kWaves > kMaxThreads)
+  k->tiles = T / k->block_rows + std::min<int64_t>(g->B, g->T);
+  k->units = k->tiles + (k->split ? (k->target + c.heads - 1) / c.heads + 2 : 0);
+  if (k->units * c.heads * 64 * kWaves * (k->split ? 8 : 1) > kMaxThreads)
     return set_error(LEECH_E_SHAPE, "too many rows for a launch");
   k->bytes = k->split ? (size_t)(c.heads * k->units * k->block_rows) * (c.dim + 2) * sizeof(float)
                       : 0;
   return LEECH_OK;
 }
 
-// Sequences of up to kFewRows rows are stream_kernel's; tile_kernel takes longer
-// ones, and all of them where no sequence need be short (T rows make B sequences
-// of max_new).
+// Sequences of up to kFewRows rows are stream_kernel's (16 at dim > 128, where two
+// tiles of them do not fit the registers); tile_kernel takes longer ones, and all
+// of them where B sequences are 256 rows long on average: few can be short then,
+// and a second launch, for most calls without work, costs 10 us.
 int cut_all(const leech_attend_args* g, const CacheShape& c, Cuts* k) {
   const int64_t group = g->q_heads / c.heads;
   const int64_t rows = std::min<int64_t>(g->max_new, g->T) * group;
   *k = {};
   int rc = LEECH_OK;
-  const bool many = rows > kFewRows;
-  const bool few = !many || g->T < (int64_t)g->B * g->max_new;
+  const int few_rows = c.dim > 128 ? 16 : kFewRows;
+  const bool many = rows > few_rows;
+  const bool few = !many || g->T * group < (int64_t)g->B * 256;
   if (few) {
-    k->few.block_rows = rows > 16 ? 32 : 16;
+    k->few.block_rows = std::min<int64_t>(rows, few_rows) > 16 ? 32 : 16;
     k->few.over = 0;
-    k->few.upto = kFewRows;
+    k->few.upto = few_rows;
     rc = cut(g, c, false, &k->few);
   }
   if (many && !rc) {
     k->many.block_rows = kTileRows;
-    k->many.over = few ? kFewRows : 0;
+    k->many.over = few ? few_rows : 0;
     k->many.upto = 0x7fffffff;
     rc = cut(g, c, true, &k->many);
   }
@@ -1099,7 +1130,8 @@ struct Launch {
 template <int CT, int DT>
 Launch pick_dim(int block_rows) {
   if (block_rows == 16) return {stream_kernel<CT, DT, 1>, 0};
-  if (block_rows == 32) return {stream_kernel<CT, DT, 2>, 0};
+  if constexpr (DT <= 128)
+    if (block_rows == 32) return {stream_kernel<CT, DT, 2>, 0};
   return {tile_kernel<CT, DT>, sizeof(TileLds<CT, DT>)};
 }
 template <int CT>
@@ -1118,6 +1150,7 @@ int launch(AttendArgs a, const Cut& k, float* workspace, hipStream_t stream) {
   a.over = k.over;
   a.upto = k.upto;
   a.target = (float)k.target;
+  a.slices = k.block_rows / 16;
   a.part_o = workspace;
   a.part_ml = workspace + (int64_t)a.c.heads * k.units * k.block_rows * a.c.dim;
   const Launch f = a.c.type == LEECH_F16    ? pick<kF16>(a.c.dim, k.block_rows)
@@ -1135,8 +1168,8 @@ int launch(AttendArgs a, const Cut& k, float* workspace, hipStream_t stream) {
   e = hipGetLastError();
   if (e != hipSuccess) return hip_fail("attend launch", e);
   if (!k.split) return LEECH_OK;
-  hipLaunchKernelGGL(join_kernel, dim3((unsigned)a.T, (unsigned)a.q_heads), dim3(64 * kWaves), 0,
-                     stream, a);
+  hipLaunchKernelGGL(join_kernel, dim3((unsigned)(k.tiles * a.c.heads * a.slices)),
+                     dim3(64 * kWaves), 0, stream, a);
   e = hipGetLastError();
   return e == hipSuccess ? LEECH_OK : hip_fail("attend join launch", e);
 }
