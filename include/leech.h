@@ -555,7 +555,7 @@ typedef struct {
  * slot holds is open.  q_heads > 0 (with a rotary) also turns q into q_out in
  * the same launch, for every token; q_out may be q itself.  Asynchronous on `stream`.
  * LEECH_E_ARG and LEECH_E_SHAPE as leech_rope, and for a cache that is not as
- * described. */
+ * described; k, v and q must be of one type (LEECH_E_ARG). */
 int leech_cache_write(const leech_kv_cache* cache, int64_t T, const leech_rows* k,
                       const leech_rows* v, const int64_t* d_slots, const int64_t* d_positions,
                       const leech_rotary* rotary, int32_t q_heads, const leech_rows* q,

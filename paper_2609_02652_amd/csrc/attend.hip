@@ -54,7 +54,7 @@ struct AttendArgs {
   float scale;                // times log2 e, its magnitude; never 0 (2^-126 stands for it)
   uint32_t flip;              // sign bits that a negative scale puts on the queries
   // how the work is cut (see the plan)
-  int32_t block_rows, log_step, min_steps, units, split;
+  int32_t block_rows, log_step, min_steps, whole_steps, units, split;
   int32_t over, upto;         // sequences of over < rows <= upto are this launch's
   int32_t slices;             // workgroups that join a tile's rows
   float target;
@@ -65,7 +65,8 @@ struct AttendArgs {
 // A sequence's rows are cut in tiles of block_rows, its keys in steps of
 // 2^log_step tokens, and the steps that a sequence's rows see in equal parts, so
 // many that all parts of all sequences together come to about `target`
-// workgroups of equal work (never less than min_steps a part).  A unit is a part
+// workgroups of equal work (never less than min_steps a part; one part up to
+// whole_steps).  A unit is a part
 // of a tile; units are numbered sequence by sequence, tile by tile.  Every wave
 // works the numbering out for itself, a lane a sequence.
 struct Sequence {
@@ -144,7 +145,7 @@ __device__ __forceinline__ bool find(const AttendArgs& a, Number what, int numbe
   int before = 0, units_before = 0;
   for (int b = 0; b < a.B; b += 64) {
     Sequence s = b ? sequence(a, b + lane) : head;
-    s.parts = a.split ? (s.steps + steps - 1) / steps : 1;
+    s.parts = s.steps > a.whole_steps ? (s.steps + steps - 1) / steps : 1;
     const int units = s.tiles * s.parts, own = what == kUnitNumber ? units : s.tiles;
     const int upto = before + wave_scan(own);
     const uint64_t mask = __ballot(number >= upto - own && number < upto);
@@ -327,7 +328,7 @@ __device__ __forceinline__ float base_for(float top, float qs, float big) {
 }
 constexpr float kSlack = 8.0f;
 
-constexpr int kWaves = 4;
+constexpr int kStreamWaves = 8, kWaves = 4;     // of a workgroup: stream_kernel's, the others'
 
 // A workgroup is a unit of up to 16·NT rows; its waves take the unit's steps in
 // turn and join at the end.  DT: the head's dimension, or the next of 64, 128,
@@ -335,15 +336,17 @@ constexpr int kWaves = 4;
 // are 32 registers a lane each at DT = 128, the next step's keys loading while
 // this one's weights and values are worked on and the other way round.
 template <int CT, int DT, int NT>
-__global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void stream_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * kStreamWaves, DT > 128 ? 1 : 2) void stream_kernel(AttendArgs a) {
   constexpr int R = kRun<CT>, TOK = kStep<CT>, NU = R / 4;
   constexpr int KC = DT * kBytes<CT> / 64;       // sixteen-byte loads of a key row's lane
   constexpr int KM = DT / 32;                    // products along a head
   constexpr int VM = DT / 16;                    // tiles of coordinates
   constexpr int H = kBytes<CT> == 2 ? 1 : 2;     // operands in sixteen bytes
-  constexpr int COLS = 64;                       // coordinates joined at once
-  __shared__ float joined[kWaves][16 * NT][COLS + 4];
-  __shared__ float stats[kWaves][16 * NT][2];
+  // coordinates joined at once: a thread four of a row
+  constexpr int COLS = 4 * (64 * kStreamWaves) / (16 * NT) < DT ? 4 * (64 * kStreamWaves) / (16 * NT) : DT;
+  __shared__ float joined[kStreamWaves][16 * NT][COLS + 4];
+  __shared__ kv_f32x2 stats[16 * NT][kStreamWaves];
+  __shared__ float inverse[16 * NT];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int h = blockIdx.x % a.c.heads, unit = blockIdx.x / a.c.heads;
   Sequence s;
@@ -360,9 +363,12 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void stream_kernel(A
   row_range(a, s, row0 + rows - 1, lo_last, hi_last);
   int step0 = lo_first / TOK, step1 = (hi_last + TOK - 1) / TOK;
   if (step1 < step0) step1 = step0;
-  const int64_t span = step1 - step0;
-  step1 = step0 + (int)(span * (part + 1) / s.parts);
-  step0 = step0 + (int)(span * part / s.parts);
+  // parts of whole rounds of the waves
+  const int share = ((step1 - step0 + s.parts - 1) / s.parts + kStreamWaves - 1) / kStreamWaves *
+                    kStreamWaves;
+  const int64_t from_step = step0 + (int64_t)part * share;
+  step1 = from_step + share < step1 ? (int)(from_step + share) : step1;
+  step0 = from_step < step1 ? (int)from_step : step1;
 
   int lo[NT], hi[NT];
   kv_u32x4 qf[NT][KM];
@@ -379,10 +385,8 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void stream_kernel(A
     for (int m = 0; m < KM; ++m) {
       // the coordinates that sixteen bytes of a key hold, in their order
       const int d = H == 1 ? 32 * m + 8 * g : 64 * (m / 2) + 16 * g + 8 * (m % 2);
-      qf[t][m] = in && d < a.c.dim ? *(const kv_u32x4*)(q + d) ^ a.flip : kv_u32x4{0, 0, 0, 0};
+      qf[t][m] = in && d < a.c.dim ? *(const kv_u32x4*)(q + d) : kv_u32x4{0, 0, 0, 0};
     }
-    qs[t] = a.scale;
-    if (H == 2 && a.type == LEECH_BF16) qs[t] = to_f16<KM, 32>(qf[t], a.scale);
   }
 
   f32x4 o[NT][VM];
@@ -455,11 +459,19 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void stream_kernel(A
     load_keys(pk, jk);
     load_scales(pv, jv);
     load_values(pv, jv);
-    int next = step + kWaves < step1 ? step + kWaves : step;
+    // (the queries have arrived with the pages; their signs and types wait for nothing)
+#pragma unroll
+    for (int x = 0; x < NT; ++x) {
+      qs[x] = a.scale;
+#pragma unroll
+      for (int k = 0; k < KM; ++k) qf[x][k] ^= a.flip;
+      if (H == 2 && a.type == LEECH_BF16) qs[x] = to_f16<KM, 32>(qf[x], a.scale);
+    }
+    int next = step + kStreamWaves < step1 ? step + kStreamWaves : step;
     jk = run_at(next, col >> 2);
     jv = run_at(next, g);
     int pk2 = page_of(jk), pv2 = page_of(jv);
-    for (;; step += kWaves) {
+    for (;; step += kStreamWaves) {
       const bool lost = pv < 0 || pv >= a.pages;       // this lane's run has no page
       f32x4 sc[NT][NU];
 #pragma unroll
@@ -474,7 +486,7 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void stream_kernel(A
 #pragma unroll
           for (int t = 0; t < NT; ++t) sc[t][u] = mfma16<CT>(x, qf[t][k], sc[t][u]);
         }
-      const bool more = step + kWaves < step1;
+      const bool more = step + kStreamWaves < step1;
       if (more) load_keys(pk2, jk);
 
       // what a row does not see, and what is not a number behind its mask
@@ -557,7 +569,7 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void stream_kernel(A
       if (!more) break;
       load_values(pv2, jv);
       pv = pv2;
-      next = step + 2 * kWaves < step1 ? step + 2 * kWaves : step + kWaves;
+      next = step + 2 * kStreamWaves < step1 ? step + 2 * kStreamWaves : step + kStreamWaves;
       jk = run_at(next, col >> 2);
       jv = run_at(next, g);
       pk2 = page_of(jk);
@@ -569,64 +581,60 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void stream_kernel(A
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     l[t] = quarters_sum(l[t]);
-    if (g == 0) {
-      stats[wave][16 * t + col][0] = base[t];
-      stats[wave][16 * t + col][1] = l[t];
-    }
+    if (g == 0) stats[16 * t + col][wave] = kv_f32x2{base[t], l[t]};
   }
   __syncthreads();
+  const bool whole = s.parts == 1;
+  const int64_t part_row = ((int64_t)h * a.units + unit) * a.block_rows;
   float f[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    float top = -__builtin_inff();
+    kv_f32x2 y[kStreamWaves];
+    float top = -__builtin_inff(), sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stats[w][16 * t + col][0]);
-    f[t] = __builtin_amdgcn_exp2f(base[t] - (top == -__builtin_inff() ? 0.0f : top));
-  }
-  const bool whole = s.parts == 1;
-  const int64_t part_row = ((int64_t)h * a.units + unit) * a.block_rows;
-  const int c4 = 4 * (threadIdx.x & 15);
-  for (int c0 = 0; c0 < a.c.dim; c0 += COLS) {
-    __syncthreads();
-#pragma unroll
-    for (int v = 0; v < VM; ++v)
-      if (16 * v >= c0 && 16 * v < c0 + COLS)
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-          *(f32x4*)&joined[wave][16 * t + col][16 * v - c0 + 4 * g] = o[t][v] * f[t];
-    __syncthreads();
-    if (c0 + c4 >= a.c.dim) continue;
-    for (int r = threadIdx.x >> 4; r < rows; r += 16) {
-      f32x4 x = {0, 0, 0, 0};
-      float top = -__builtin_inff(), sum = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        x += *(const f32x4*)&joined[w][r][c4];
-        top = fmaxf(top, stats[w][r][0]);
-      }
-      const float base = top == -__builtin_inff() ? 0.0f : top;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w)
-        sum += stats[w][r][1] * __builtin_amdgcn_exp2f(stats[w][r][0] - base);
-      if (!whole) {
-        *(f32x4*)(a.part_o + (part_row + r) * a.c.dim + c0 + c4) = x;
-        if (c0 + c4 == 0) {
-          a.part_ml[2 * (part_row + r)] = top;
-          a.part_ml[2 * (part_row + r) + 1] = sum;
-        }
-        continue;
-      }
-      const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;     // a NaN sum stays one
-      x *= inv;
-      const int64_t t = s.first + (row0 + r) / a.group;
-      const int qh = h * a.group + (row0 + r) % a.group;
-      const bool half = a.type == LEECH_F16;
-      *(kv_u32x2*)(a.out + t * a.o_token + qh * a.o_head + c0 + c4) =
-          half ? kv_u32x2{pack2<kF16>(x[0], x[1]), pack2<kF16>(x[2], x[3])}
-               : kv_u32x2{pack2<kBf16>(x[0], x[1]), pack2<kBf16>(x[2], x[3])};
-      if (a.lse && c0 + c4 == 0)
-        a.lse[t * a.q_heads + qh] = sum != 0.0f ? (top + log2f(sum)) * kLn2 : -__builtin_inff();
+    for (int w = 0; w < kStreamWaves; ++w) {
+      y[w] = stats[16 * t + col][w];
+      top = fmaxf(top, y[w][0]);
     }
+    const float to = top == -__builtin_inff() ? 0.0f : top;
+    f[t] = __builtin_amdgcn_exp2f(base[t] - to);
+    if (wave == t && g == 0 && 16 * t + col < rows) {
+#pragma unroll
+      for (int w = 0; w < kStreamWaves; ++w) sum += y[w][1] * __builtin_amdgcn_exp2f(y[w][0] - to);
+      const int r = 16 * t + col;
+      inverse[r] = whole ? (sum != 0.0f ? 1.0f / sum : 0.0f) : 1.0f;     // a NaN sum stays one
+      if (!whole)
+        *(kv_f32x2*)(a.part_ml + 2 * (part_row + r)) = kv_f32x2{top, sum};
+      else if (a.lse)
+        a.lse[(s.first + (row0 + r) / a.group) * a.q_heads + h * a.group + (row0 + r) % a.group] =
+            sum != 0.0f ? (top + log2f(sum)) * kLn2 : -__builtin_inff();
+    }
+  }
+#pragma unroll
+  for (int c0 = 0; c0 < DT; c0 += COLS) {
+    if (c0 >= a.c.dim) break;
+    if (c0) __syncthreads();
+#pragma unroll
+    for (int v = c0 / 16; v < (c0 + COLS) / 16; ++v)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        *(f32x4*)&joined[wave][16 * t + col][16 * v - c0 + 4 * g] = o[t][v] * f[t];
+    __syncthreads();
+    const int r = threadIdx.x / (COLS / 4), c = 4 * (threadIdx.x % (COLS / 4));
+    if (r >= rows || c0 + c >= a.c.dim) continue;
+    f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < kStreamWaves; ++w) x += *(const f32x4*)&joined[w][r][c];
+    x *= inverse[r];
+    if (!whole) {
+      *(f32x4*)(a.part_o + (part_row + r) * a.c.dim + c0 + c) = x;
+      continue;
+    }
+    const int64_t t = s.first + (row0 + r) / a.group;
+    const int qh = h * a.group + (row0 + r) % a.group;
+    *(kv_u32x2*)(a.out + t * a.o_token + qh * a.o_head + c0 + c) =
+        a.type == LEECH_F16 ? kv_u32x2{pack2<kF16>(x[0], x[1]), pack2<kF16>(x[2], x[3])}
+                            : kv_u32x2{pack2<kBf16>(x[0], x[1]), pack2<kBf16>(x[2], x[3])};
   }
 }
 
@@ -969,10 +977,11 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
     a.lse[t * a.q_heads + qh] = l != 0.0f ? (base + log2f(l)) * kLn2 : -__builtin_inff();
 }
 
-// Joins the parts of a unit's rows: a workgroup is a tile of one sequence and cache
-// head, a wave a row at a time.  A row's parts are weighed first, a lane a part,
-// then summed, a lane four coordinates, with no load waiting for another.
+// Joins the parts of a tile's rows: a wave a row, or, where there are more parts
+// than its eight loads at once take, a workgroup a row.  A wave weighs all parts,
+// a lane a part, then sums its share of them, a lane four coordinates.
 __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a) {
+  __shared__ f32x4 quarter[kWaves][kMaxHeadDim / 4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int h = blockIdx.x % a.c.heads;
   const int slice = blockIdx.x / a.c.heads % a.slices, at_tile = blockIdx.x / a.c.heads / a.slices;
@@ -985,15 +994,18 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a) {
   const int row0 = tile * a.block_rows;
   const int rows = s.rows - row0 < a.block_rows ? s.rows - row0 : a.block_rows;
   const int64_t first = ((int64_t)h * a.units + u0 + tile * s.parts) * a.block_rows;
-  const int lanes = a.c.dim / 4;                       // of a part's row
-  const int each = lanes <= 16 ? 4 : lanes <= 32 ? 2 : 1;   // parts that a wave reads at once
+  const int each = a.c.dim <= 64 ? 4 : a.c.dim <= 128 ? 2 : 1;      // parts a wave reads at once
   const int sub = lane / (64 / each), c = 4 * (lane % (64 / each));
   const bool in = c < a.c.dim;
-  for (int r = slice * kWaves + wave; r < rows; r += kWaves * a.slices) {
+  constexpr int U = 8;
+  const int team = s.parts > U * each ? kWaves : 1, member = wave % team;     // waves of a row
+  for (int r = (slice * kWaves + wave) / team; r < rows; r += a.slices * (kWaves / team)) {
     const int64_t at = first + r;
+    const auto ml = [&](int p) {
+      return *(const kv_f32x2*)(a.part_ml + 2 * (at + (int64_t)p * a.block_rows));
+    };
     float top = -__builtin_inff();
-    for (int p = lane; p < s.parts; p += 64)
-      top = fmaxf(top, a.part_ml[2 * (at + (int64_t)p * a.block_rows)]);
+    for (int p = lane; p < s.parts; p += 64) top = fmaxf(top, ml(p)[0]);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
     const float base = top == -__builtin_inff() ? 0.0f : top;
@@ -1002,16 +1014,25 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a) {
     for (int p0 = 0; p0 < s.parts; p0 += 64) {
       float f = 0.0f;
       if (p0 + lane < s.parts) {
-        const kv_f32x2 y = *(const kv_f32x2*)(a.part_ml + 2 * (at + (int64_t)(p0 + lane) * a.block_rows));
+        const kv_f32x2 y = ml(p0 + lane);
         f = __builtin_amdgcn_exp2f(y[0] - base);
         sum += f * y[1];
       }
       const int n = s.parts - p0 < 64 ? s.parts - p0 : 64;
-#pragma unroll 8
-      for (int p = 0; p < n; p += each) {
-        const float w = __shfl(f, p + sub, 64);
-        if (in && p + sub < n)
-          x += *(const f32x4*)(a.part_o + (at + (int64_t)(p0 + p + sub) * a.block_rows) * a.c.dim + c) * w;
+      for (int p = member * each; p < n; p += U * team * each) {
+        f32x4 y[U];
+        float w[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = p + u * team * each + sub, k = i < n ? i : n - 1;
+          y[u] = *(const f32x4*)(a.part_o + (at + (int64_t)(p0 + k) * a.block_rows) * a.c.dim +
+                                 (in ? c : 0));
+          w[u] = __shfl(f, k, 64);
+          w[u] = i < n ? w[u] : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (w[u] != 0.0f) x += y[u] * w[u];          // (a part that saw nothing may hold anything)
       }
     }
 #pragma unroll
@@ -1019,14 +1040,21 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a) {
     for (int d = 64 / each; d < 64; d <<= 1)
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] += __shfl_xor(x[e], d, 64);
+    if (team > 1) {
+      __syncthreads();
+      if (in && sub == 0) quarter[wave][c / 4] = x;
+      __syncthreads();
+      if (wave == 0 && in)
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) x += quarter[w][c / 4];
+    }
+    if (member || !in || sub) continue;
     const int64_t t = s.first + (row0 + r) / a.group;
     const int qh = h * a.group + (row0 + r) % a.group;
-    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;       // a NaN sum stays one
-    x *= inv;
-    if (in && sub == 0)
-      *(kv_u32x2*)(a.out + t * a.o_token + qh * a.o_head + c) =
-          a.type == LEECH_F16 ? kv_u32x2{pack2<kF16>(x[0], x[1]), pack2<kF16>(x[2], x[3])}
-                              : kv_u32x2{pack2<kBf16>(x[0], x[1]), pack2<kBf16>(x[2], x[3])};
+    x *= sum != 0.0f ? 1.0f / sum : 0.0f;              // a NaN sum stays one
+    *(kv_u32x2*)(a.out + t * a.o_token + qh * a.o_head + c) =
+        a.type == LEECH_F16 ? kv_u32x2{pack2<kF16>(x[0], x[1]), pack2<kF16>(x[2], x[3])}
+                            : kv_u32x2{pack2<kBf16>(x[0], x[1]), pack2<kBf16>(x[2], x[3])};
     if (a.lse && lane == 0)
       a.lse[t * a.q_heads + qh] = sum != 0.0f ? (top + log2f(sum)) * kLn2 : -__builtin_inff();
   }
@@ -1035,12 +1063,13 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a) {
 // ------------------------------------------------------------------ host side
 constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;
 constexpr int kFewRows = 32;           // rows of a sequence that stream_kernel takes
-constexpr int kTargetFew = 1024, kTargetMany = 512;   // workgroups that split sequences come to
-constexpr int kMinTokens = 256;        // keys of a part, at least
+constexpr int kTargetFew = 512, kTargetMany = 512;    // workgroups that split sequences come to
+constexpr int kMinTokens = 256;        // keys of a part of many rows, at least
+constexpr int kWholeTokens = 1024;     // keys that are not worth a second launch
 
 // One launch's share of a call: a function of sizes alone.
 struct Cut {
-  int block_rows, log_step, min_steps, split, over, upto, target;
+  int waves, block_rows, log_step, min_steps, whole_steps, split, over, upto, target;
   int64_t tiles, units;
   size_t bytes;
 };
@@ -1053,13 +1082,16 @@ int cut(const leech_attend_args* g, const CacheShape& c, bool many, Cut* k) {
   const int64_t keys = (int64_t)g->table_pages << c.log_page;
   k->target = many ? kTargetMany : kTargetFew;
   k->log_step = many ? (c.dim > 128 ? 5 : 6) : type_bytes(c.type) == 2 ? 5 : 6;
-  k->min_steps = kMinTokens >> k->log_step;
+  k->min_steps = many ? kMinTokens >> k->log_step : kStreamWaves;
   const int64_t least = (T + k->block_rows - 1) / k->block_rows;
-  k->split = keys > kMinTokens && least * c.heads < k->target;
+  k->whole_steps = kWholeTokens >> k->log_step;
+  k->split = keys > kWholeTokens && least * c.heads < k->target;
+  if (!k->split) k->whole_steps = 0x7fffffff;
+  k->waves = many ? kWaves : kStreamWaves;
   // (two more for the roundings of the plan's f32 total)
   k->tiles = T / k->block_rows + std::min<int64_t>(g->B, g->T);
   k->units = k->tiles + (k->split ? (k->target + c.heads - 1) / c.heads + 2 : 0);
-  if (k->units * c.heads * 64 * kWaves * (k->split ? 8 : 1) > kMaxThreads)
+  if (k->units * c.heads * 64 * k->waves > kMaxThreads)
     return set_error(LEECH_E_SHAPE, "too many rows for a launch");
   k->bytes = k->split ? (size_t)(c.heads * k->units * k->block_rows) * (c.dim + 2) * sizeof(float)
                       : 0;
@@ -1145,12 +1177,15 @@ int launch(AttendArgs a, const Cut& k, float* workspace, hipStream_t stream) {
   a.block_rows = k.block_rows;
   a.log_step = k.log_step;
   a.min_steps = k.min_steps;
+  a.whole_steps = k.whole_steps;
   a.units = (int32_t)k.units;
   a.split = k.split;
   a.over = k.over;
   a.upto = k.upto;
   a.target = (float)k.target;
-  a.slices = k.block_rows / 16;
+  // a row a wave, unless that makes more workgroups than the card takes at once
+  a.slices = (int32_t)std::max<int64_t>(
+      1, std::min<int64_t>(k.block_rows / kWaves, 4096 / (k.tiles * a.c.heads)));
   a.part_o = workspace;
   a.part_ml = workspace + (int64_t)a.c.heads * k.units * k.block_rows * a.c.dim;
   const Launch f = a.c.type == LEECH_F16    ? pick<kF16>(a.c.dim, k.block_rows)
@@ -1163,8 +1198,8 @@ int launch(AttendArgs a, const Cut& k, float* workspace, hipStream_t stream) {
                             (int)f.lds);
     if (e != hipSuccess) return hip_fail("hipFuncSetAttribute", e);
   }
-  hipLaunchKernelGGL(f.fn, dim3((unsigned)(a.c.heads * k.units)), dim3(64 * kWaves), f.lds, stream,
-                     a);
+  hipLaunchKernelGGL(f.fn, dim3((unsigned)(a.c.heads * k.units)), dim3(64 * k.waves), f.lds,
+                     stream, a);
   e = hipGetLastError();
   if (e != hipSuccess) return hip_fail("attend launch", e);
   if (!k.split) return LEECH_OK;

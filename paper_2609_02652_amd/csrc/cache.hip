@@ -13,14 +13,18 @@
 // coordinate, which is what a lane of the attention's second matrix product
 // takes, so that it reads them from memory as they are.
 //
-// Geometry.  Teams of sixteen lanes own a row (one head of one token), a lane
-// eight coordinates at a time: four pairs where the rotation reaches.  A team
-// keeps its token and walks over heads, so a sine is computed once for several
-// of them.  Value rows go through LDS, tile by tile of consecutive tokens: where
-// value_run tokens fill a run of slots the tile writes sixteen bytes at once,
-// anywhere else element by element.
+// Geometry.  Teams of sixteen lanes own a key or query row (one head of one token),
+// a lane eight coordinates at a time: four pairs where the rotation reaches.  A
+// team keeps its token and walks over heads, four rows loading at once, so a sine
+// is computed once for several of them.  A wave owns the values of a few
+// consecutive tokens and one head.  Where tokens fill a run of slots it takes the
+// run whole: half of the wave half of the run's tokens, a lane four coordinates of
+// each, so that the run's sixteen bytes a coordinate are put together (or taken
+// apart) in the lane's registers.  Elsewhere it goes token by token.
 
 #include "kv_device.h"
+
+#include <type_traits>
 
 namespace leech {
 namespace {
@@ -28,8 +32,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kTeam = 16;                 // lanes of a row
 constexpr int kTeams = kThreads / kTeam;
-constexpr int kItems = kMaxHeadDim / 8 / kTeam;   // eights of coordinates a lane owns
-constexpr int kSpare = 15;                // tokens a tile reads past its own
+constexpr int kWaves = kThreads / 64;
+constexpr int kAtOnce = 4;                // rows a team has on their way
 
 struct Rows {
   void* data;
@@ -55,7 +59,7 @@ struct WriteArgs {
   int32_t q_heads, k_heads;               // rows of q, then of k, that a token turns
   int32_t by_token;                       // teams of a block: as many tokens, or heads of one
   int32_t slice, slices;                  // heads of a block; blocks of a token's heads
-  int32_t tile;                           // tokens of a value tile
+  int32_t tokens;                         // of a wave's values
 };
 
 struct ReadArgs {
@@ -65,35 +69,43 @@ struct ReadArgs {
   const int64_t* slots;
   Rows k, v;
   int64_t T, key_blocks;
-  int32_t tile;
+  int32_t tokens;
 };
 
-__device__ __forceinline__ void load4(const Rows& r, int64_t at, float v[4]) {
-  if (r.type == LEECH_F32) {
-    const float* p = (const float*)r.data + at;
-    if (r.wide) {
-      const kv_f32x4 w = *(const kv_f32x4*)p;
+// Four elements as they lie: an f32 each, or two 16-bit ones a word.
+template <int SRC>
+using Four = typename std::conditional<SRC == LEECH_F32, kv_u32x4, kv_u32x2>::type;
+template <int SRC>
+__device__ __forceinline__ Four<SRC> load4(const Rows& r, int64_t at) {
+  Four<SRC> w;
+  if constexpr (SRC == LEECH_F32) {
+    const uint32_t* p = (const uint32_t*)r.data + at;
+    if (r.wide)
+      w = *(const kv_u32x4*)p;
+    else
 #pragma unroll
-      for (int t = 0; t < 4; ++t) v[t] = w[t];
-    } else {
-#pragma unroll
-      for (int t = 0; t < 4; ++t) v[t] = p[t];
-    }
-    return;
-  }
-  const uint16_t* p = (const uint16_t*)r.data + at;
-  uint32_t h[4];
-  if (r.wide) {
-    const kv_u32x2 w = *(const kv_u32x2*)p;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) h[t] = w[t >> 1] >> (16 * (t & 1)) & 0xFFFFu;
+      for (int t = 0; t < 4; ++t) w[t] = p[t];
   } else {
+    const uint16_t* p = (const uint16_t*)r.data + at;
+    if (r.wide)
+      w = *(const kv_u32x2*)p;
+    else
 #pragma unroll
-    for (int t = 0; t < 4; ++t) h[t] = p[t];
+      for (int t = 0; t < 2; ++t) w[t] = p[2 * t] | (uint32_t)p[2 * t + 1] << 16;
   }
-  const bool half = r.type == LEECH_F16;
+  return w;
+}
+template <int SRC>
+__device__ __forceinline__ void values4(const Four<SRC>& w, float v[4]) {
 #pragma unroll
-  for (int t = 0; t < 4; ++t) v[t] = half ? half_value(h[t]) : bf16_value(h[t]);
+  for (int t = 0; t < 4; ++t) {
+    if constexpr (SRC == LEECH_F32)
+      v[t] = __builtin_bit_cast(float, (uint32_t)w[t]);
+    else if constexpr (SRC == LEECH_F16)
+      v[t] = half_value(w[t >> 1] >> (16 * (t & 1)));
+    else
+      v[t] = bf16_value(w[t >> 1] >> (16 * (t & 1)) & 0xFFFFu);
+  }
 }
 
 __device__ __forceinline__ uint32_t bits16(int type, float v) {
@@ -167,10 +179,11 @@ __device__ __forceinline__ void rotate8(const Turn& t, float lo[4], float hi[4],
   }
 }
 
-// Largest magnitude over a team's lanes, NaN if any value is not finite.
-__device__ __forceinline__ float team_largest(float v) {
+// Largest magnitude over groups of N lanes, NaN if any value is not finite.
+template <int N>
+__device__ __forceinline__ float group_largest(float v) {
 #pragma unroll
-  for (int m = 1; m < kTeam; m <<= 1) {
+  for (int m = 1; m < N; m <<= 1) {
     const float o = __shfl_xor(v, m, 64);
     v = o > v || o != o ? o : v;
   }
@@ -207,23 +220,25 @@ __device__ __forceinline__ float code_value(int type, uint32_t code) {
 }
 
 // ------------------------------------------------------------------- writing
-// A key row into its slot.
-__device__ __forceinline__ void keep_key(const WriteArgs& a, int64_t slot, int h, int n_items,
-                                         int lane, float lo[kItems][4], float hi[kItems][4]) {
+// A key row into its slot; a lane holds eights lane and lane + 16 (ITEMS = 2).
+template <int ITEMS>
+__device__ __forceinline__ void keep_key(const WriteArgs& a, int64_t slot, int h, int lane,
+                                         float lo[ITEMS][4], float hi[ITEMS][4]) {
+  const int n_items = a.c.dim / 8;
   const int64_t base = key_at(a.c, slot, h);
   float scale = 0.0f;
   if (type_bytes(a.c.type) == 1) {
     float m = 0.0f;
 #pragma unroll
-    for (int g = 0; g < kItems; ++g)
+    for (int g = 0; g < ITEMS; ++g)
       if (lane + g * kTeam < n_items)
 #pragma unroll
         for (int t = 0; t < 4; ++t) m = larger(larger(m, lo[g][t]), hi[g][t]);
-    scale = code_scale(a.c.type, team_largest(m));
+    scale = code_scale(a.c.type, group_largest<kTeam>(m));
     if (lane == 0) a.sk[scale_at(a.c, slot, h)] = scale;
   }
 #pragma unroll
-  for (int g = 0; g < kItems; ++g) {
+  for (int g = 0; g < ITEMS; ++g) {
     const int item = lane + g * kTeam;
     if (item >= n_items) break;
     int d0, d1;
@@ -239,6 +254,7 @@ __device__ __forceinline__ void keep_key(const WriteArgs& a, int64_t slot, int h
   }
 }
 
+template <int SRC, int ITEMS>
 __device__ __forceinline__ void turn_block(const WriteArgs& a, int64_t block) {
   const int team = threadIdx.x / kTeam, lane = threadIdx.x % kTeam;
   const int n_items = a.c.dim / 8;
@@ -249,248 +265,324 @@ __device__ __forceinline__ void turn_block(const WriteArgs& a, int64_t block) {
   const int first = (int)part * a.slice + (a.by_token ? 0 : team);
   const int all = a.q_heads + a.k_heads;
   const int last = (int)part * a.slice + a.slice < all ? (int)part * a.slice + a.slice : all;
-  float c[kItems][4], s[kItems][4];
-#pragma unroll
-  for (int g = 0; g < kItems; ++g)
-    if (8 * (lane + g * kTeam) < a.turn.width)
-      angles(a.turn, a.positions[t], lane + g * kTeam, c[g], s[g]);
   int64_t slot = -1;
   if (a.k_heads) slot = a.slots[t];
-  for (int h = first; h < last; h += step) {
-    const bool key = h >= a.q_heads;
-    if (key && (slot < 0 || slot >= a.c.slots)) continue;
-    const Rows& from = key ? a.k : a.q;
-    const int64_t at = t * from.token + (key ? h - a.q_heads : h) * from.head;
-    float lo[kItems][4], hi[kItems][4];
+  const bool kept = slot >= 0 && slot < a.c.slots;
+  int d0[ITEMS], d1[ITEMS];
 #pragma unroll
-    for (int g = 0; g < kItems; ++g) {
-      const int item = lane + g * kTeam;
-      if (item >= n_items) continue;
-      int d0, d1;
-      item_coords(a.turn, item, d0, d1);
-      load4(from, at + d0, lo[g]);
-      load4(from, at + d1, hi[g]);
-    }
-#pragma unroll
-    for (int g = 0; g < kItems; ++g)
-      if (8 * (lane + g * kTeam) < a.turn.width) rotate8(a.turn, lo[g], hi[g], c[g], s[g]);
-    if (key) {
-      keep_key(a, slot, h - a.q_heads, n_items, lane, lo, hi);
-      continue;
-    }
-    const int64_t to = t * a.qo.token + h * a.qo.head;
-#pragma unroll
-    for (int g = 0; g < kItems; ++g) {
-      const int item = lane + g * kTeam;
-      if (item >= n_items) continue;
-      int d0, d1;
-      item_coords(a.turn, item, d0, d1);
-      store4(a.qo, to + d0, lo[g]);
-      store4(a.qo, to + d1, hi[g]);
-    }
+  for (int g = 0; g < ITEMS; ++g) {
+    const int item = lane + g * kTeam;
+    item_coords(a.turn, item < n_items ? item : 0, d0[g], d1[g]);
   }
-}
-
-// Whether tokens t .. t + run - 1 exist and fill a run of slots that starts at
-// slot (of token t), itself the first place of a run.
-__device__ __forceinline__ bool fills_run(const int64_t* slots, int64_t T, int64_t all, int64_t t,
-                                          int run) {
-  if (t < 0 || t + run > T) return false;
-  const int64_t s = slots[t];
-  if (s < 0 || s + run > all || (s & (run - 1))) return false;
-  for (int j = 1; j < run; ++j)
-    if (slots[t + j] != s + j) return false;
-  return true;
-}
-
-// Value rows of a tile of tokens and one head.  A tile writes the runs that
-// start at its own tokens (it reads up to run - 1 tokens past them for that)
-// and those of its tokens that lie in no filled run.
-__device__ __forceinline__ void value_block(const WriteArgs& a, int64_t block, uint8_t* tile) {
-  const int team = threadIdx.x / kTeam, lane = threadIdx.x % kTeam;
-  const int size = type_bytes(a.c.type), run = value_run(a.c.type);
-  const int dim = a.c.dim, n_items = dim / 8, pitch = dim * size + 4;
-  const int h = (int)(block % a.c.heads);
-  const int64_t t0 = block / a.c.heads * a.tile;
-  const int own = (int)(a.T - t0 < a.tile ? a.T - t0 : a.tile);
-  const int held = (int)(a.T - t0 < own + run - 1 ? a.T - t0 : own + run - 1);
-  // per token: whether it starts a run that its tile writes whole (1), or is
-  // written by itself (2), or lies in such a run (0)
-  uint8_t* how = tile + (a.tile + kSpare) * pitch;
-  for (int i = threadIdx.x; i < own; i += kThreads) {
-    const int64_t t = t0 + i, slot = a.slots[t];
-    const int place = (int)(slot & (run - 1));
-    uint8_t w = 0;
-    if (slot >= 0 && slot < a.c.slots) {
-      if (!fills_run(a.slots, a.T, a.c.slots, t - place, run))
-        w = 2;
-      else if (place == 0)
-        w = 1;
-    }
-    how[i] = w;
-  }
-  for (int i = team; i < held; i += kTeams) {
-    const int64_t t = t0 + i, slot = a.slots[t];
-    if (slot < 0 || slot >= a.c.slots) continue;
-    const int64_t at = t * a.v.token + h * a.v.head;
-    float v[kItems][8];
-    float m = 0.0f;
+  float c[ITEMS][4], s[ITEMS][4];
+  for (int h0 = first; h0 < last; h0 += kAtOnce * step) {
+    Four<SRC> lo[kAtOnce][ITEMS], hi[kAtOnce][ITEMS];
 #pragma unroll
-    for (int g = 0; g < kItems; ++g) {
-      const int item = lane + g * kTeam;
-      if (item >= n_items) continue;
-      load4(a.v, at + 8 * item, v[g]);
-      load4(a.v, at + 8 * item + 4, v[g] + 4);
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int h = h0 + u * step;
+      if (h >= last) break;
+      const bool key = h >= a.q_heads;
+      const Rows& from = key ? a.k : a.q;
+      const int64_t at = t * from.token + (key ? h - a.q_heads : h) * from.head;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) m = larger(m, v[g][e]);
-    }
-    float scale = 0.0f;
-    if (size == 1) {
-      scale = code_scale(a.c.type, team_largest(m));
-      if (lane == 0 && i < own) a.sv[scale_at(a.c, slot, h)] = scale;
-    }
-#pragma unroll
-    for (int g = 0; g < kItems; ++g) {
-      const int item = lane + g * kTeam;
-      if (item >= n_items) continue;
-      uint32_t* to = (uint32_t*)(tile + i * pitch + 8 * item * size);
-      if (size == 1) {
-        to[0] = codes4(a.c.type, v[g], scale);
-        to[1] = codes4(a.c.type, v[g] + 4, scale);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          to[e] = bits16(a.c.type, v[g][2 * e]) | bits16(a.c.type, v[g][2 * e + 1]) << 16;
+      for (int g = 0; g < ITEMS; ++g) {
+        lo[u][g] = load4<SRC>(from, at + d0[g]);
+        hi[u][g] = load4<SRC>(from, at + d1[g]);
       }
     }
-  }
-  __syncthreads();
-  const int wave = threadIdx.x / 64, l = threadIdx.x % 64;
-  for (int i = wave; i < own; i += kThreads / 64) {
-    const int w = how[i];
-    if (w == 0) continue;
-    const int64_t base = value_at(a.c, a.slots[t0 + i], h);
-    for (int d = l; d < dim; d += 64) {
-      const uint8_t* from = tile + i * pitch + d * size;
-      if (w == 2) {
-        if (size == 1)
-          a.cv[base + (int64_t)d * run] = *from;
-        else
-          *(uint16_t*)(a.cv + 2 * (base + (int64_t)d * run)) = *(const uint16_t*)from;
+    if (h0 == first)                     // while the first rows are on their way
+#pragma unroll
+      for (int g = 0; g < ITEMS; ++g)
+        if (8 * (lane + g * kTeam) < a.turn.width)
+          angles(a.turn, a.positions[t], lane + g * kTeam, c[g], s[g]);
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int h = h0 + u * step;
+      if (h >= last) break;
+      float vl[ITEMS][4], vh[ITEMS][4];
+#pragma unroll
+      for (int g = 0; g < ITEMS; ++g) {
+        values4<SRC>(lo[u][g], vl[g]);
+        values4<SRC>(hi[u][g], vh[g]);
+        if (8 * (lane + g * kTeam) < a.turn.width) rotate8(a.turn, vl[g], vh[g], c[g], s[g]);
+      }
+      if (h >= a.q_heads) {
+        if (kept) keep_key<ITEMS>(a, slot, h - a.q_heads, lane, vl, vh);
         continue;
       }
-      kv_u32x4 o;
+      const int64_t to = t * a.qo.token + h * a.qo.head;
+#pragma unroll
+      for (int g = 0; g < ITEMS; ++g)
+        if (lane + g * kTeam < n_items) {
+          store4(a.qo, to + d0[g], vl[g]);
+          store4(a.qo, to + d1[g], vh[g]);
+        }
+    }
+  }
+}
+
+// The slots around a wave's tokens: lane L has that of token t0 − 16 + L (−1 past
+// either end).  Bit L of `joins`: lane L's slot follows lane L − 1's in its run;
+// of `heads`: it is the first place of a run.
+struct Neighbours {
+  int64_t slot;
+  uint64_t joins, heads;
+};
+__device__ __forceinline__ Neighbours neighbours(const int64_t* slots, int64_t T, int64_t all,
+                                                 int64_t t0, int run) {
+  const int lane = threadIdx.x & 63;
+  const int64_t t = t0 - 16 + lane;
+  int64_t slot = t >= 0 && t < T ? slots[t] : -1;
+  if (slot >= all) slot = -1;
+  const int64_t before = __shfl_up(slot, 1, 64);
+  const bool inner = slot >= 0 && (slot & (run - 1)) != 0;
+  return {slot, __ballot(inner && lane > 0 && slot == before + 1),
+          __ballot(slot >= 0 && (slot & (run - 1)) == 0)};
+}
+// Whether a whole run starts at lane `at`.
+__device__ __forceinline__ bool whole_run(const Neighbours& n, int at, int run) {
+  const uint64_t rest = ((1ull << (run - 1)) - 1) << (at + 1);
+  return (n.heads >> at & 1) && (n.joins & rest) == rest;
+}
+__device__ __forceinline__ int64_t lane_slot(const Neighbours& n, int at) {
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(n.slot >> 32), at) << 32 |
+                   (uint32_t)__builtin_amdgcn_readlane((int)n.slot, at));
+}
+
+// Values of `tokens` tokens and one head, a wave.  A whole run belongs to the wave
+// of its first token; a token of no whole run to its own.
+template <int SRC, int ITEMS>
+__device__ __forceinline__ void value_wave(const WriteArgs& a, int64_t group) {
+  const int lane = threadIdx.x & 63, size = type_bytes(a.c.type), run = value_run(a.c.type);
+  const int h = (int)(group % a.c.heads);
+  const int64_t t0 = group / a.c.heads * a.tokens;
+  if (t0 >= a.T) return;
+  const Neighbours n = neighbours(a.slots, a.T, a.c.slots, t0, run);
+  const int end = 16 + (int)(a.T - t0 < a.tokens ? a.T - t0 : a.tokens);
+  for (int at = 16; at < end; ++at) {
+    const int64_t slot = lane_slot(n, at);
+    if (slot < 0) continue;
+    const int64_t t = t0 + at - 16;
+    const int place = (int)(slot & (run - 1));
+    if (place && at >= place && whole_run(n, at - place, run)) continue;    // another's
+    if (place == 0 && whole_run(n, at, run)) {
+      const int half = lane >> 5, d = 4 * (lane & 31), mine = run / 2;
+      const int64_t base = value_at(a.c, slot, h) * size + 8 * half;
+      constexpr int J = 8;
+      Four<SRC> w[J][ITEMS];
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int g = 0; g < ITEMS; ++g) {
+          const int dd = d + 128 * g;
+          if (j < mine)
+            w[j][g] = load4<SRC>(a.v, (t + half * mine + j) * a.v.token + h * a.v.head +
+                                          (dd < a.c.dim ? dd : 0));
+        }
       if (size == 1) {
+        float scale[J];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          uint32_t x = 0;
+        for (int j = 0; j < J; ++j) {
+          float m = 0.0f;
 #pragma unroll
-          for (int b = 0; b < 4; ++b) x |= (uint32_t)from[(4 * e + b) * pitch] << (8 * b);
-          o[e] = x;
+          for (int g = 0; g < ITEMS; ++g) {
+            float v[4];
+            values4<SRC>(w[j][g], v);
+            if (d + 128 * g < a.c.dim)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) m = larger(m, v[e]);
+          }
+          scale[j] = code_scale(a.c.type, group_largest<32>(m));
+        }
+        if ((lane & 31) == 0) {
+          float* to = a.sv + scale_at(a.c, slot, h) + 8 * half;
+          *(kv_f32x4*)to = kv_f32x4{scale[0], scale[1], scale[2], scale[3]};
+          *(kv_f32x4*)(to + 4) = kv_f32x4{scale[4], scale[5], scale[6], scale[7]};
+        }
+#pragma unroll
+        for (int g = 0; g < ITEMS; ++g) {
+          if (d + 128 * g >= a.c.dim) break;
+          kv_u32x2 o[4] = {{0, 0}, {0, 0}, {0, 0}, {0, 0}};
+#pragma unroll
+          for (int j = 0; j < J; ++j) {
+            float v[4];
+            values4<SRC>(w[j][g], v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e][j >> 2] |= code_of(a.c.type, v[e], scale[j]) << (8 * (j & 3));
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) *(kv_u32x2*)(a.cv + base + 16 * (d + 128 * g + e)) = o[e];
         }
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          o[e] = (uint32_t) * (const uint16_t*)(from + 2 * e * pitch) |
-                 (uint32_t) * (const uint16_t*)(from + (2 * e + 1) * pitch) << 16;
+        for (int g = 0; g < ITEMS; ++g) {
+          if (d + 128 * g >= a.c.dim) break;
+          kv_u32x2 o[4] = {{0, 0}, {0, 0}, {0, 0}, {0, 0}};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float v[4];
+            values4<SRC>(w[j][g], v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e][j >> 1] |= bits16(a.c.type, v[e]) << (16 * (j & 1));
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) *(kv_u32x2*)(a.cv + base + 16 * (d + 128 * g + e)) = o[e];
+        }
       }
-      *(kv_u32x4*)(a.cv + size * (base + (int64_t)d * run)) = o;
+      continue;
+    }
+    // one token: a lane four coordinates
+    const int d = 4 * lane;
+    float v[4];
+    values4<SRC>(load4<SRC>(a.v, t * a.v.token + h * a.v.head + (d < a.c.dim ? d : 0)), v);
+    float scale = 0.0f;
+    if (size == 1) {
+      float m = 0.0f;
+      if (d < a.c.dim)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = larger(m, v[e]);
+      scale = code_scale(a.c.type, group_largest<64>(m));
+      if (lane == 0) a.sv[scale_at(a.c, slot, h)] = scale;
+    }
+    if (d >= a.c.dim) continue;
+    const int64_t base = value_at(a.c, slot, h) + (int64_t)d * run;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (size == 1)
+        a.cv[base + e * run] = (uint8_t)code_of(a.c.type, v[e], scale);
+      else
+        ((uint16_t*)a.cv)[base + e * run] = (uint16_t)bits16(a.c.type, v[e]);
     }
   }
 }
 
+template <int SRC, int ITEMS>
 __global__ __launch_bounds__(kThreads) void write_kernel(WriteArgs a) {
-  extern __shared__ __attribute__((aligned(16))) uint8_t tile[];
   if ((int64_t)blockIdx.x < a.turn_blocks)
-    turn_block(a, blockIdx.x);
+    turn_block<SRC, ITEMS>(a, blockIdx.x);
   else
-    value_block(a, blockIdx.x - a.turn_blocks, tile);
+    value_wave<SRC, ITEMS>(a, (blockIdx.x - a.turn_blocks) * kWaves + threadIdx.x / 64);
 }
 
 // ------------------------------------------------------------------- reading
-__device__ __forceinline__ void values8(int type, const uint8_t* p, float v[8]) {
-  if (type_bytes(type) == 1) {
-    const kv_u32x2 w = *(const kv_u32x2*)p;
+// Eight keys' numbers.
+__device__ __forceinline__ void values8(int type, const kv_u32x4& w, float scale, float v[8]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = code_value(type, w[e >> 2] >> (8 * (e & 3)) & 0xFFu);
-  } else {
-    const kv_u32x4 w = *(const kv_u32x4*)p;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
+  for (int e = 0; e < 8; ++e) {
+    if (type_bytes(type) == 1) {
+      v[e] = code_value(type, w[e >> 2] >> (8 * (e & 3)) & 0xFFu) * scale;
+    } else {
       const uint32_t h = w[e >> 1] >> (16 * (e & 1)) & 0xFFFFu;
       v[e] = type == LEECH_F16 ? half_value(h) : bf16_value(h);
     }
   }
 }
 
-__device__ __forceinline__ void put_row(const ReadArgs& a, const Rows& to, int64_t t, int h,
-                                        bool valid, const uint8_t* row, float scale, int lane) {
+__device__ __forceinline__ void read_keys(const ReadArgs& a, int64_t block) {
+  const int team = threadIdx.x / kTeam, lane = threadIdx.x % kTeam;
   const int size = type_bytes(a.c.type);
-  const int64_t at = t * to.token + h * to.head;
-  for (int item = lane; item < a.c.dim / 8; item += kTeam) {
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (valid) {
-      values8(a.c.type, row + 8 * item * size, v);
-      if (size == 1)
+  const int64_t rows = a.T * a.c.heads, first = block * kTeams * kAtOnce + team;
+  int64_t slot[kAtOnce];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= scale;
+  for (int u = 0; u < kAtOnce; ++u) {
+    const int64_t row = first + u * kTeams;
+    slot[u] = a.slots[(row < rows ? row : first < rows ? first : 0) / a.c.heads];
+    if (slot[u] >= a.c.slots) slot[u] = -1;
+  }
+  for (int item = lane; item < a.c.dim / 8; item += kTeam) {
+    kv_u32x4 w[kAtOnce];
+    float scale[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int64_t row = first + u * kTeams;
+      const int h = (int)(row % a.c.heads);
+      const int64_t at = scale_at(a.c, slot[u] < 0 ? 0 : slot[u], h);
+      const uint8_t* p = a.ck + (at * a.c.dim + 8 * item) * size;
+      w[u] = kv_u32x4{0, 0, 0, 0};
+      scale[u] = 1.0f;
+      if (size == 1) {
+        const kv_u32x2 x = *(const kv_u32x2*)p;
+        w[u] = kv_u32x4{x[0], x[1], 0, 0};
+        scale[u] = a.sk[at];
+      } else {
+        w[u] = *(const kv_u32x4*)p;
+      }
     }
-    store4(to, at + 8 * item, v);
-    store4(to, at + 8 * item + 4, v + 4);
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int64_t row = first + u * kTeams;
+      if (row >= rows) break;
+      float v[8];
+      values8(a.c.type, w[u], scale[u], v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = slot[u] < 0 ? 0.0f : v[e];
+      const int64_t to = row / a.c.heads * a.k.token + row % a.c.heads * a.k.head + 8 * item;
+      store4(a.k, to, v);
+      store4(a.k, to + 4, v + 4);
+    }
+  }
+}
+
+// Values of `tokens` tokens (up to 32) and one head, a wave: run by run, as far as
+// consecutive tokens lie in one; half the wave each half of the run's sixteen bytes.
+__device__ __forceinline__ void read_values(const ReadArgs& a, int64_t group) {
+  const int lane = threadIdx.x & 63, size = type_bytes(a.c.type), run = value_run(a.c.type);
+  const int h = (int)(group % a.c.heads);
+  const int64_t t0 = group / a.c.heads * a.tokens;
+  if (t0 >= a.T) return;
+  const Neighbours n = neighbours(a.slots, a.T, a.c.slots, t0, run);
+  const int end = 16 + (int)(a.T - t0 < a.tokens ? a.T - t0 : a.tokens);
+  const int half = lane >> 5;
+  for (int at = 16; at < end;) {
+    const int64_t slot = lane_slot(n, at);
+    int count = 1;
+    if (slot >= 0)
+      while (at + count < end && (n.joins >> (at + count) & 1)) ++count;
+    const int place = slot < 0 ? half * (run / 2) : (int)(slot & (run - 1));
+    const int64_t row = t0 + at - 16;
+    at += count;
+    const int64_t first = slot < 0 ? 0 : slot - place;
+    float scale[8] = {1, 1, 1, 1, 1, 1, 1, 1};
+    if (size == 1) {
+      const float* p = a.sv + scale_at(a.c, first, h) + 8 * half;
+      const kv_f32x4 x = *(const kv_f32x4*)p, y = *(const kv_f32x4*)(p + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        scale[e] = x[e];
+        scale[4 + e] = y[e];
+      }
+    }
+    const uint8_t* base = a.cv + value_at(a.c, first, h) * size + 8 * half;
+    for (int d = 4 * (lane & 31); d < a.c.dim; d += 128) {
+      kv_u32x2 w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = *(const kv_u32x2*)(base + 16 * (d + e));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int e0 = half * (run / 2) + j - place;       // the token's, counted from the first
+        if (j >= run / 2 || e0 < 0 || e0 >= count) continue;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (size == 1) {
+            v[e] = code_value(a.c.type, w[e][j >> 2] >> (8 * (j & 3)) & 0xFFu) * scale[j];
+          } else {
+            const uint32_t x = w[e][(j >> 1) & 1] >> (16 * (j & 1)) & 0xFFFFu;
+            v[e] = a.c.type == LEECH_F16 ? half_value(x) : bf16_value(x);
+          }
+          if (slot < 0) v[e] = 0.0f;
+        }
+        store4(a.v, (row + e0) * a.v.token + h * a.v.head + d, v);
+      }
+    }
   }
 }
 
 __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a) {
-  extern __shared__ __attribute__((aligned(16))) uint8_t tile[];
-  const int team = threadIdx.x / kTeam, lane = threadIdx.x % kTeam;
-  const int size = type_bytes(a.c.type), run = value_run(a.c.type), dim = a.c.dim;
-  if ((int64_t)blockIdx.x < a.key_blocks) {
-    const int64_t row = (int64_t)blockIdx.x * kTeams + team;
-    if (row >= a.T * a.c.heads) return;
-    const int64_t t = row / a.c.heads;
-    const int h = (int)(row % a.c.heads);
-    const int64_t slot = a.slots[t];
-    const bool valid = slot >= 0 && slot < a.c.slots;
-    put_row(a, a.k, t, h, valid, valid ? a.ck + size * key_at(a.c, slot, h) : nullptr,
-            valid && size == 1 ? a.sk[scale_at(a.c, slot, h)] : 0.0f, lane);
-    return;
-  }
-  const int64_t block = blockIdx.x - a.key_blocks;
-  const int h = (int)(block % a.c.heads);
-  const int64_t t0 = block / a.c.heads * a.tile;
-  const int own = (int)(a.T - t0 < a.tile ? a.T - t0 : a.tile);
-  const int pitch = dim * size + 16;
-  // A token leads if it does not lie behind its predecessor in one run; the
-  // leader reads the run's sixteen bytes for those that follow it there.
-  const int wave = threadIdx.x / 64, l = threadIdx.x % 64;
-  for (int i = wave; i < own; i += kThreads / 64) {
-    const int64_t slot = a.slots[t0 + i];
-    if (slot < 0 || slot >= a.c.slots) continue;
-    const int place = (int)(slot & (run - 1));
-    if (i > 0 && place > 0 && a.slots[t0 + i - 1] == slot - 1) continue;
-    int n = 1;
-    while (place + n < run && i + n < own && a.slots[t0 + i + n] == slot + n) ++n;
-    const int64_t base = value_at(a.c, slot - place, h);
-    for (int d = l; d < dim; d += 64) {
-      const kv_u32x4 w = *(const kv_u32x4*)(a.cv + size * (base + (int64_t)d * run));
-      for (int j = 0; j < n; ++j) {
-        const int e = place + j;
-        uint8_t* to = tile + (i + j) * pitch + d * size;
-        const uint32_t x = e * size < 4 ? w[0] : e * size < 8 ? w[1] : e * size < 12 ? w[2] : w[3];
-        if (size == 1)
-          *to = (uint8_t)(x >> (8 * (e & 3)));
-        else
-          *(uint16_t*)to = (uint16_t)(x >> (16 * (e & 1)));
-      }
-    }
-  }
-  __syncthreads();
-  for (int i = team; i < own; i += kTeams) {
-    const int64_t t = t0 + i, slot = a.slots[t];
-    const bool valid = slot >= 0 && slot < a.c.slots;
-    put_row(a, a.v, t, h, valid, tile + i * pitch,
-            valid && size == 1 ? a.sv[scale_at(a.c, slot, h)] : 0.0f, lane);
-  }
+  if ((int64_t)blockIdx.x < a.key_blocks)
+    read_keys(a, blockIdx.x);
+  else
+    read_values(a, (blockIdx.x - a.key_blocks) * kWaves + threadIdx.x / 64);
 }
 
 // ------------------------------------------------------------------ host side
@@ -540,6 +632,25 @@ void share_out(WriteArgs* a) {
   a->slices = (heads + a->slice - 1) / a->slice;
   a->token_blocks = a->by_token ? (a->T + kTeams - 1) / kTeams : a->T;
   a->turn_blocks = heads ? a->token_blocks * a->slices : 0;
+}
+
+template <int SRC>
+int launch_type(const WriteArgs& a, int64_t blocks, hipStream_t stream) {
+  if (a.c.dim <= 8 * kTeam)
+    hipLaunchKernelGGL((write_kernel<SRC, 1>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((write_kernel<SRC, 2>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
+  return 0;
+}
+int launch_write(const WriteArgs& a, int src, int64_t blocks, const char* what, void* stream) {
+  if (src == LEECH_F32)
+    launch_type<LEECH_F32>(a, blocks, (hipStream_t)stream);
+  else if (src == LEECH_F16)
+    launch_type<LEECH_F16>(a, blocks, (hipStream_t)stream);
+  else
+    launch_type<LEECH_BF16>(a, blocks, (hipStream_t)stream);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? LEECH_OK : hip_fail(what, e);
 }
 
 }  // namespace
@@ -603,10 +714,7 @@ extern "C" int leech_rope(int64_t T, int32_t heads, int32_t dim, const leech_row
   a.q_heads = heads;
   share_out(&a);
   if (a.turn_blocks > kMaxBlocks) return set_error(LEECH_E_SHAPE, "too many rows for a launch");
-  hipLaunchKernelGGL(write_kernel, dim3((unsigned)a.turn_blocks), dim3(kThreads), 0,
-                     (hipStream_t)stream, a);
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? LEECH_OK : hip_fail("rope launch", e);
+  return launch_write(a, a.q.type, a.turn_blocks, "rope launch", stream);
 }
 
 extern "C" int leech_cache_write(const leech_kv_cache* cache, int64_t T, const leech_rows* k,
@@ -635,6 +743,8 @@ extern "C" int leech_cache_write(const leech_kv_cache* cache, int64_t T, const l
        (rc = rows_of("q_out", q_out, T, q_heads, dim, &a.qo)) ||
        (rc = own_rows("q_out", a.qo, T, q_heads, dim))))
     return rc;
+  if (a.k.type != a.v.type || (q_heads > 0 && a.q.type != a.k.type))
+    return set_error(LEECH_E_ARG, "k, v and q must be of one type");
   a.ck = (uint8_t*)cache->k;
   a.cv = (uint8_t*)cache->v;
   a.sk = cache->k_scale;
@@ -644,15 +754,14 @@ extern "C" int leech_cache_write(const leech_kv_cache* cache, int64_t T, const l
   a.T = T;
   a.q_heads = q_heads;
   a.k_heads = heads;
-  a.tile = T < 256 ? 16 : 64;
+  // a token a wave while waves are few; eight (a run of 16-bit values) make a whole
+  // run likely to be one wave's
+  a.tokens = T < 512 ? 1 : 8;
   share_out(&a);
-  const int64_t blocks = a.turn_blocks + (T + a.tile - 1) / a.tile * heads;
-  if (blocks > kMaxBlocks) return set_error(LEECH_E_SHAPE, "too many rows for a launch");
-  const size_t lds = (size_t)(a.tile + kSpare) * (dim * type_bytes(a.c.type) + 4) + a.tile;
-  hipLaunchKernelGGL(write_kernel, dim3((unsigned)blocks), dim3(kThreads), lds,
-                     (hipStream_t)stream, a);
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? LEECH_OK : hip_fail("cache write launch", e);
+  const int64_t blocks = a.turn_blocks + ((T + a.tokens - 1) / a.tokens * heads + kWaves - 1) / kWaves;
+  if (T > kMaxBlocks || blocks > kMaxBlocks)
+    return set_error(LEECH_E_SHAPE, "too many rows for a launch");
+  return launch_write(a, a.k.type, blocks, "cache write launch", stream);
 }
 
 extern "C" int leech_cache_read(const leech_kv_cache* cache, int64_t T, const int64_t* d_slots,
@@ -676,14 +785,12 @@ extern "C" int leech_cache_read(const leech_kv_cache* cache, int64_t T, const in
   a.sv = cache->v_scale;
   a.slots = d_slots;
   a.T = T;
-  a.tile = T < 256 ? 16 : 64;
-  a.key_blocks = (T * heads + kTeams - 1) / kTeams;
-  const int64_t blocks = a.key_blocks + (T + a.tile - 1) / a.tile * heads;
+  a.tokens = T < 512 ? 1 : 16;
+  a.key_blocks = (T * heads + kTeams * kAtOnce - 1) / (kTeams * kAtOnce);
+  const int64_t blocks = a.key_blocks + ((T + a.tokens - 1) / a.tokens * heads + kWaves - 1) / kWaves;
   if (T > kMaxBlocks || blocks > kMaxBlocks)
     return set_error(LEECH_E_SHAPE, "too many rows for a launch");
-  const size_t lds = (size_t)a.tile * (dim * type_bytes(a.c.type) + 16);
-  hipLaunchKernelGGL(read_kernel, dim3((unsigned)blocks), dim3(kThreads), lds,
-                     (hipStream_t)stream, a);
+  hipLaunchKernelGGL(read_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, (hipStream_t)stream, a);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? LEECH_OK : hip_fail("cache read launch", e);
 }

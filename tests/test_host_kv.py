@@ -88,6 +88,8 @@ def test_rope_refuses(args, code):
     ((cache(), -1, rows(), rows(), FAKE, None, None, 0, None, None), SHAPE),
     ((cache(), 4, None, rows(), FAKE, None, None, 0, None, None), ARG),
     ((cache(), 4, rows(), rows(0), FAKE, None, None, 0, None, None), ARG),
+    ((cache(), 4, rows(), rows(type=_lib.F32), FAKE, None, None, 0, None, None), ARG),
+    ((cache(), 4, rows(), rows(), FAKE, FAKE, rotary(), 2, rows(type=_lib.BF16), rows()), ARG),
     ((cache(), 4, rows(), rows(), None, None, None, 0, None, None), ARG),
     ((cache(), 4, rows(), rows(), FAKE, None, rotary(), 0, None, None), ARG),   # no positions
     ((cache(), 4, rows(), rows(), FAKE, None, None, 2, rows(), rows()), ARG),   # q without rotary
