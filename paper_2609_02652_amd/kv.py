@@ -36,13 +36,19 @@ def _types():
     return _TYPES
 
 
+_HERE = nullcontext()
+
+
 def _on(device, stream):
     """(context to run a call in, its stream's handle)."""
     torch = _torch()
     if stream is None:
-        if device.index == torch.cuda.current_device():
-            return nullcontext(), torch._C._cuda_getCurrentRawStream(device.index)
-        return torch.cuda.device(device), torch._C._cuda_getCurrentRawStream(device.index)
+        handle = torch._C._cuda_getCurrentRawStream(device.index)
+        # (cheaper than torch.cuda.current_device(), which sees to the set-up that a
+        # GPU tensor has had)
+        if device.index == torch._C._cuda_getDevice():
+            return _HERE, handle
+        return torch.cuda.device(device), handle
     if not hasattr(stream, "cuda_stream"):
         handle = int(stream)
         # (an ExternalStream of 0 would be a new stream)
@@ -58,24 +64,23 @@ def _gpu(name, t, device=None):
         raise ValueError(f"{name} must be on {device or 'a GPU'}, not on {t.device}")
 
 
-def _rows(name, x, shape=None, device=None):
-    """leech_rows of a [T, heads, dim] tensor with unit stride along a head."""
+def _rows(name, x, shape, device):
+    """leech_rows of a tensor `shape` = (T, heads, dim) with unit stride along a head."""
     kind = _types().get(x.dtype)
-    if kind not in (_lib.F32, _lib.F16, _lib.BF16) or x.dim() != 3:
-        raise ValueError(f"{name} must be an f32, f16 or bf16 tensor [T, heads, dim]")
-    if shape is not None and tuple(x.shape) != tuple(shape):
-        raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(x.shape)}")
+    if kind is None or kind > _lib.BF16 or x.shape != shape:
+        raise ValueError(f"{name} must be an f32, f16 or bf16 tensor {list(shape)}, "
+                         f"not {x.dtype} {list(x.shape)}")
     ts, hs, ds = x.stride()
-    if ds != 1 and x.shape[2] != 1:
+    if ds != 1:
         raise ValueError(f"{name} must have unit stride along a head")
-    _gpu(name, x, device)
+    if x.device != device:
+        raise ValueError(f"{name} must be on {device}, not on {x.device}")
     return _lib.Rows(x.data_ptr(), kind, ts, hs)
 
 
 def _index(name, t, dtype, n, device):
-    if t.dtype != dtype or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} entries")
-    _gpu(name, t, device)
+    if t.dtype != dtype or t.shape != (n,) or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} entries on {device}")
     return t.data_ptr()
 
 
@@ -138,18 +143,23 @@ def rope(x, positions, rotary: Rotary, out=None, dtype=None, transpose=False, st
     positions int64 [T] -> a tensor of `dtype` (x's if None), or `out`, which may
     be x.  transpose: by the opposite angles (the gradient's pass)."""
     torch = _torch()
-    cx = _rows("x", x)
-    T, heads, dim = x.shape
-    pos = _index("positions", positions, torch.int64, T, x.device)
-    _gpu("rotary", rotary.freq, x.device)
+    if x.dim() != 3:
+        raise ValueError("x must be a tensor [T, heads, dim]")
+    _gpu("x", x)
+    shape, dev = x.shape, x.device
+    T, heads, dim = shape
+    cx = _rows("x", x, shape, dev)
+    pos = _index("positions", positions, torch.int64, T, dev)
+    if rotary.device != dev:
+        raise ValueError(f"the rotary must be on {dev}, not on {rotary.device}")
     if out is not None and dtype is not None and out.dtype != dtype:
         raise ValueError("out has another dtype than asked for")
-    ctx, handle = _on(x.device, stream)
+    ctx, handle = _on(dev, stream)
     with ctx:
         if out is None:
-            out = torch.empty((T, heads, dim), dtype=dtype or x.dtype, device=x.device)
-        _lib.rope(T, heads, dim, cx, pos, rotary._c, transpose,
-                  _rows("out", out, x.shape, x.device), handle)
+            out = torch.empty(shape, dtype=dtype or x.dtype, device=dev)
+        _lib.rope(T, heads, dim, cx, pos, rotary._c, transpose, _rows("out", out, shape, dev),
+                  handle)
     return out
 
 
@@ -212,37 +222,36 @@ class KVCache:
         With q [T, q_heads, dim], the same launch turns q into `out` (or a new
         tensor of `dtype`, q's if None) and returns it."""
         torch = _torch()
-        T = k.shape[0]
+        T, dev = k.shape[0], self.device
         shape = (T, self.heads, self.dim)
-        ck, cv = _rows("k", k, shape, self.device), _rows("v", v, shape, self.device)
-        at = _index("slots", slots, torch.int64, T, self.device)
+        ck, cv = _rows("k", k, shape, dev), _rows("v", v, shape, dev)
+        at = _index("slots", slots, torch.int64, T, dev)
         if (rotary is None) != (positions is None):
             raise ValueError("a rotary and positions come together")
-        pos = None
+        pos = turn = cq = None
         if rotary is not None:
-            pos = _index("positions", positions, torch.int64, T, self.device)
-            _gpu("rotary", rotary.freq, self.device)
-        if q is None:
-            if out is not None or dtype is not None:
-                raise ValueError("out and dtype are of the turned q")
-            ctx, handle = _on(self.device, stream)
-            with ctx:
-                _lib.cache_write(self._c, T, ck, cv, at, pos, rotary and rotary._c, 0, None, None,
-                                 handle)
-            return None
-        if rotary is None:
-            raise ValueError("q is only turned: it needs a rotary")
-        cq = _rows("q", q, (T, q.shape[1] if q.dim() == 3 else 0, self.dim), self.device)
-        if q.shape[1] == 0:
-            raise ValueError("q has no heads")
-        if out is not None and dtype is not None and out.dtype != dtype:
-            raise ValueError("out has another dtype than asked for")
-        ctx, handle = _on(self.device, stream)
+            pos, turn = _index("positions", positions, torch.int64, T, dev), rotary._c
+            if rotary.device != dev:
+                raise ValueError(f"the rotary must be on {dev}, not on {rotary.device}")
+        q_heads = 0
+        if q is not None:
+            if rotary is None:
+                raise ValueError("q is only turned: it needs a rotary")
+            if q.dim() != 3 or q.shape[1] == 0:
+                raise ValueError("q must be a tensor [T, q_heads, dim]")
+            q_heads = q.shape[1]
+            q_shape = (T, q_heads, self.dim)
+            cq = _rows("q", q, q_shape, dev)
+            if out is not None and dtype is not None and out.dtype != dtype:
+                raise ValueError("out has another dtype than asked for")
+        elif out is not None or dtype is not None:
+            raise ValueError("out and dtype are of the turned q")
+        ctx, handle = _on(dev, stream)
         with ctx:
-            if out is None:
-                out = torch.empty(tuple(q.shape), dtype=dtype or q.dtype, device=self.device)
-            _lib.cache_write(self._c, T, ck, cv, at, pos, rotary._c, q.shape[1], cq,
-                             _rows("out", out, q.shape, self.device), handle)
+            if q is not None and out is None:
+                out = torch.empty(q_shape, dtype=dtype or q.dtype, device=dev)
+            _lib.cache_write(self._c, T, ck, cv, at, pos, turn, q_heads, cq,
+                             None if q is None else _rows("out", out, q_shape, dev), handle)
         return out
 
     def read(self, slots, dtype=None, out=None, stream=None):
@@ -260,8 +269,8 @@ class KVCache:
             elif dtype is not None and any(t.dtype != dtype for t in out):
                 raise ValueError("out has another dtype than asked for")
             k, v = out
-            _lib.cache_read(self._c, T, at, _rows("k", k, shape, self.device),
-                            _rows("v", v, shape, self.device), handle)
+            ck, cv = _rows("k", k, shape, self.device), _rows("v", v, shape, self.device)
+            _lib.cache_read(self._c, T, at, ck, cv, handle)
         return k, v
 
     def attend(self, q, page_table, kv_len, q_start=None, max_new=None, causal=True, window=0,
@@ -280,37 +289,36 @@ class KVCache:
         if kind not in (_lib.F16, _lib.BF16) or q.dim() != 3 or q.shape[2] != self.dim:
             raise ValueError(f"q must be an f16 or bf16 tensor [T, q_heads, {self.dim}]")
         dev = self.device
-        _gpu("q", q, dev)
         T, heads, dim = q.shape
-        if page_table.dim() != 2 or page_table.dtype != torch.int32 or (
-                page_table.shape[1] > 1 and page_table.stride(1) != 1):
-            raise ValueError("page_table must be an int32 tensor [B, pages], contiguous along a row")
-        _gpu("page_table", page_table, dev)
-        B, width = page_table.shape
+        if page_table.dim() != 2 or page_table.dtype != torch.int32:
+            raise ValueError("page_table must be an int32 tensor [B, pages]")
+        (B, width), (apart, along) = page_table.shape, page_table.stride()
+        if along != 1 and width > 1:
+            raise ValueError("page_table must be contiguous along a row")
+        if q.device != dev or page_table.device != dev:
+            raise ValueError(f"q and page_table must be on {dev}")
         lens = _index("kv_len", kv_len, torch.int32, B, dev)
-        starts = None if q_start is None else _index("q_start", q_start, torch.int32, B + 1, dev)
-        if q_start is None and T != B:
+        starts = None
+        if q_start is not None:
+            starts = _index("q_start", q_start, torch.int32, B + 1, dev)
+        elif T != B:
             raise ValueError("without q_start there is one new token a sequence")
-        qs, os_ = q.stride(), None
+        qs = q.stride()
         if qs[2] != 1:
             raise ValueError("q must have unit stride along a head")
-        if out is not None:
-            if out.dtype != q.dtype or out.shape != q.shape:
-                raise ValueError("out must have q's type and shape")
-            os_ = out.stride()
-            if os_[2] != 1:
-                raise ValueError("out must have unit stride along a head")
-            _gpu("out", out, dev)
+        if out is not None and (out.dtype != q.dtype or out.shape != q.shape
+                                or out.stride(2) != 1 or out.device != dev):
+            raise ValueError("out must have q's type, shape and device and unit stride along a head")
         ctx, handle = _on(dev, stream)
         with ctx:
             if out is None:
                 out = torch.empty((T, heads, dim), dtype=q.dtype, device=dev)
-                os_ = out.stride()
+            os_ = out.stride()
             lse = torch.empty((T, heads), dtype=torch.float32, device=dev) if with_lse else None
             args = _lib.AttendArgs(
                 kind, heads, T, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1],
                 lse.data_ptr() if with_lse else None, B, starts, lens, page_table.data_ptr(),
-                page_table.stride(0), width,
+                apart, width,
                 (1 if q_start is None else T) if max_new is None else max_new, int(causal), window,
                 dim ** -0.5 if scale is None else scale, None, 0)
             size = _lib.attend_workspace(self._c, args)
