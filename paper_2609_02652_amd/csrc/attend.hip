@@ -428,9 +428,6 @@ __global__ __launch_bounds__(64 * kStreamWaves, DT > 128 ? 1 : 2) void stream_ke
   const auto load_values = [&](int page, int j) {
     const int64_t at = place(page, j);
     const uint8_t* run = a.cv + at * row_bytes + 16 * col;
-#pragma unroll
-    for (int v = 0; v < VM; ++v)
-      if (16 * v < a.c.dim) vw[v] = *(const kv_u32x4*)(run + 256 * v);
     if constexpr (H == 2) {
 #pragma unroll
       for (int e = 0; e < R; e += 4) {
@@ -439,6 +436,9 @@ __global__ __launch_bounds__(64 * kStreamWaves, DT > 128 ? 1 : 2) void stream_ke
         for (int r = 0; r < 4; ++r) vs[e + r] = x[r];
       }
     }
+#pragma unroll
+    for (int v = 0; v < VM; ++v)
+      if (16 * v < a.c.dim) vw[v] = *(const kv_u32x4*)(run + 256 * v);
   };
   const auto load_scales = [&](int page, int j) {
     if constexpr (H == 2) {
@@ -467,9 +467,13 @@ __global__ __launch_bounds__(64 * kStreamWaves, DT > 128 ? 1 : 2) void stream_ke
       for (int k = 0; k < KM; ++k) qf[x][k] ^= a.flip;
       if (H == 2 && a.type == LEECH_BF16) qs[x] = to_f16<KM, 32>(qf[x], a.scale);
     }
-    int next = step + kStreamWaves < step1 ? step + kStreamWaves : step;
-    jk = run_at(next, col >> 2);
-    jv = run_at(next, g);
+    // the pages of a step are asked for a step ahead of its keys: loads come back in
+    // their order, so what waits for a page must not have asked for more before it
+    const auto after = [&](int st, int n) {
+      return st + n * kStreamWaves < step1 ? st + n * kStreamWaves : st;
+    };
+    jk = run_at(after(step, 1), col >> 2);
+    jv = run_at(after(step, 1), g);
     int pk2 = page_of(jk), pv2 = page_of(jv);
     for (;; step += kStreamWaves) {
       const bool lost = pv < 0 || pv >= a.pages;       // this lane's run has no page
@@ -487,7 +491,14 @@ __global__ __launch_bounds__(64 * kStreamWaves, DT > 128 ? 1 : 2) void stream_ke
           for (int t = 0; t < NT; ++t) sc[t][u] = mfma16<CT>(x, qf[t][k], sc[t][u]);
         }
       const bool more = step + kStreamWaves < step1;
-      if (more) load_keys(pk2, jk);
+      int jk3 = jk, jv3 = jv, pk3 = pk2, pv3 = pv2;
+      if (more) {
+        jk3 = run_at(after(step + kStreamWaves, 1), col >> 2);
+        jv3 = run_at(after(step + kStreamWaves, 1), g);
+        pk3 = page_of(jk3);
+        pv3 = page_of(jv3);
+        load_keys(pk2, jk);
+      }
 
       // what a row does not see, and what is not a number behind its mask
       const int t0 = step * TOK;
@@ -569,11 +580,10 @@ __global__ __launch_bounds__(64 * kStreamWaves, DT > 128 ? 1 : 2) void stream_ke
       if (!more) break;
       load_values(pv2, jv);
       pv = pv2;
-      next = step + 2 * kStreamWaves < step1 ? step + 2 * kStreamWaves : step + kStreamWaves;
-      jk = run_at(next, col >> 2);
-      jv = run_at(next, g);
-      pk2 = page_of(jk);
-      pv2 = page_of(jv);
+      jk = jk3;
+      jv = jv3;
+      pk2 = pk3;
+      pv2 = pv3;
     }
   }
 
@@ -666,7 +676,7 @@ struct TileLds {
   kv_u32x4 v[2][TOK * DT / 8];
   float ks[2][TOK], vs[2][TOK], big[2];
   uint32_t bad[3][TOK / 8];
-  int64_t where[4][TOK / 16];       // slot of each sixteen tokens
+  int64_t where[4][TOK / 16], slot[4][TOK / 16];    // byte, and slot, of each sixteen tokens
 };
 
 // A workgroup is a unit of up to 128 rows, a wave 32 of them; all share the keys
@@ -744,20 +754,23 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
   const int32_t* table = a.table + b * a.table_stride;
   const int first16 = lo_first & ~15, last16 = (hi_last - 1) & ~15;
   // Where sixteen tokens lie (clamped to those that are seen), by the thread of
-  // each eight of a tile; those of no page count as without numbers.
-  int64_t slot = 0;
-  uint32_t lost = 0;
+  // each eight of a tile; those of no page count as without numbers.  The page is
+  // asked for ahead of the tile's own loads and looked at behind them.
+  int page = 0, spot = 0;
   const auto look_up = [&](int step) {
-    int j = step * TOK + 16 * (tid >> 1);
-    j = j < first16 ? first16 : j > last16 ? last16 : j;
-    const int p = table[j >> a.c.log_page];
-    lost = p < 0 || p >= a.pages ? 0xFFu : 0u;
-    slot = (((int64_t)(lost ? 0 : p) * a.c.heads + h) << a.c.log_page) +
-           (j & ((1 << a.c.log_page) - 1));
+    spot = step * TOK + 16 * (tid >> 1);
+    spot = spot < first16 ? first16 : spot > last16 ? last16 : spot;
+    page = table[spot >> a.c.log_page];
   };
   const auto note = [&](int step) {
-    lds.bad[step % 3][tid] = lost;
-    if (!(tid & 1)) lds.where[step & 3][tid >> 1] = slot;
+    const bool lost = page < 0 || page >= a.pages;
+    const int64_t slot = (((int64_t)(lost ? 0 : page) * a.c.heads + h) << a.c.log_page) +
+                         (spot & ((1 << a.c.log_page) - 1));
+    lds.bad[step % 3][tid] = lost ? 0xFFu : 0u;
+    if (!(tid & 1)) {
+      lds.where[step & 3][tid >> 1] = slot * row_bytes;
+      if (CODES) lds.slot[step & 3][tid >> 1] = slot;
+    }
   };
   kv_u32x4 kw[NL], vw[NL];
   float sc = 0.0f;
@@ -768,15 +781,15 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int at = i * 64 * kWaves + tid, t = at / LC, c = at % LC;
-      kw[i] = *(const kv_u32x4*)(a.ck + (where[t >> 4] + (t & 15)) * row_bytes +
+      kw[i] = *(const kv_u32x4*)(a.ck + where[t >> 4] + (t & 15) * row_bytes +
                                  (16 * c < row_bytes ? 16 * c : 0));
       const int run = at / DT, d = at % DT;
-      vw[i] = *(const kv_u32x4*)(a.cv + (where[run * R >> 4] + (run * R & 15)) * row_bytes +
+      vw[i] = *(const kv_u32x4*)(a.cv + where[run * R >> 4] + (run * R & 15) * row_bytes +
                                  16 * (d < a.c.dim ? d : 0));
     }
     if constexpr (CODES) {
       const int t = tid & (TOK - 1);
-      sc = ((tid & TOK) ? a.sv : a.sk)[where[t >> 4] + (t & 15)];
+      sc = ((tid & TOK) ? a.sv : a.sk)[lds.slot[step & 3][t >> 4] + (t & 15)];
     }
   };
   const auto keep = [&](int step) {
@@ -833,8 +846,8 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
     const int buf = step & 1, t0 = step * TOK;
     const bool more = step + 1 < step1;
     if (more) {
-      load(step + 1);
       if (tid < TOK / 8) look_up(step + 2);
+      load(step + 1);
     }
     if (live && t0 < whi && t0 + TOK > wlo) {
       f32x16 x[NK];
