@@ -328,6 +328,14 @@ __device__ __forceinline__ float base_for(float top, float qs, float big) {
 }
 constexpr float kSlack = 8.0f;
 
+// Largest of three, numbers before NaN.  (fmaxf first makes every operand canonical,
+// an instruction each: what the products return already is.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
+}
+
 constexpr int kStreamWaves = 8, kWaves = 4;     // of a workgroup: stream_kernel's, the others'
 
 // A workgroup is a unit of up to 16·NT rows; its waves take the unit's steps in
@@ -539,9 +547,9 @@ __global__ __launch_bounds__(64 * kStreamWaves, DT > 128 ? 1 : 2) void stream_ke
           }
           if constexpr (H == 2) big = quarters_max(big);
         }
-        float top = x[0];
+        float top = -__builtin_inff();
 #pragma unroll
-        for (int e = 1; e < R; ++e) top = fmaxf(top, x[e]);
+        for (int e = 0; e < R; e += 2) top = max3(top, x[e], x[e + 1]);
         const float want = base_for<H == 2>(quarters_max(top), qs[t], big);
         if (__any(want > base[t] + kSlack)) {
           // (each row by its own scores alone, whatever its neighbours do)
@@ -667,7 +675,7 @@ constexpr int kTileTokens = DT > 128 ? 32 : 64;
 
 // LDS of the tile kernel: two buffers of keys and values (as the products take
 // them, two bytes an element), of their scales and the largest value scale; for
-// three tiles which tokens have no number for a value, or no page; for four where
+// three tiles which tokens have no number for a value, or no page; for eight where
 // the tokens lie.
 template <int CT, int DT>
 struct TileLds {
@@ -676,7 +684,8 @@ struct TileLds {
   kv_u32x4 v[2][TOK * DT / 8];
   float ks[2][TOK], vs[2][TOK], big[2];
   uint32_t bad[3][TOK / 8];
-  int64_t where[4][TOK / 16], slot[4][TOK / 16];    // byte, and slot, of each sixteen tokens
+  int64_t where[8][TOK / 16], slot[8][TOK / 16];    // byte, and slot, of each sixteen tokens
+  uint32_t lost[8][TOK / 16];                       // set where there is no such page
 };
 
 // A workgroup is a unit of up to 128 rows, a wave 32 of them; all share the keys
@@ -698,6 +707,7 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
   constexpr int LC = DT * S / 16;              // sixteen-byte loads of a key row
   constexpr int NL = TOK * LC / (64 * kWaves); // of a thread, for keys; as many for values
   constexpr bool CODES = S == 1;
+  constexpr int A = CODES && DT == 128 ? 2 : 3;   // LDS reads ahead of a product (more spill)
   extern __shared__ __attribute__((aligned(16))) uint8_t raw[];
   TileLds<CT, DT>& lds = *reinterpret_cast<TileLds<CT, DT>*>(raw);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -753,12 +763,13 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
   const int row_bytes = a.c.dim * S;
   const int32_t* table = a.table + b * a.table_stride;
   const int first16 = lo_first & ~15, last16 = (hi_last - 1) & ~15;
-  // Where sixteen tokens lie (clamped to those that are seen), by the thread of
-  // each eight of a tile; those of no page count as without numbers.  The page is
-  // asked for ahead of the tile's own loads and looked at behind them.
+  // Where sixteen tokens lie (clamped to those that are seen), four tiles at a time, a
+  // thread sixteen tokens.  Pages are asked for ahead of a tile's own loads and
+  // looked at behind them.
+  constexpr int G = TOK / 16;
   int page = 0, spot = 0;
   const auto look_up = [&](int step) {
-    spot = step * TOK + 16 * (tid >> 1);
+    spot = step * TOK + 16 * tid;
     spot = spot < first16 ? first16 : spot > last16 ? last16 : spot;
     page = table[spot >> a.c.log_page];
   };
@@ -766,62 +777,72 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
     const bool lost = page < 0 || page >= a.pages;
     const int64_t slot = (((int64_t)(lost ? 0 : page) * a.c.heads + h) << a.c.log_page) +
                          (spot & ((1 << a.c.log_page) - 1));
-    lds.bad[step % 3][tid] = lost ? 0xFFu : 0u;
-    if (!(tid & 1)) {
-      lds.where[step & 3][tid >> 1] = slot * row_bytes;
-      if (CODES) lds.slot[step & 3][tid >> 1] = slot;
-    }
+    const int to = (step + tid / G) & 7;
+    lds.where[to][tid % G] = slot * row_bytes;
+    if (CODES) lds.slot[to][tid % G] = slot;
+    lds.lost[to][tid % G] = lost ? 0xFFu : 0u;
   };
-  kv_u32x4 kw[NL], vw[NL];
-  float sc = 0.0f;
+  // Tokens of no page count as without numbers.
+  const auto clear = [&](int step) {
+    lds.bad[step % 3][tid] = lds.lost[step & 7][tid >> 1];
+  };
+  // A tile's loads and LDS writes come in 2·NL pieces, keys first, to be spread among
+  // the products: eight waves that ask for all of theirs at once wait for each other.
   // Columns past the head's dimension read others again: those of the queries are 0,
   // those of out are not kept.
-  const auto load = [&](int step) {
-    const int64_t* where = lds.where[step & 3];
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int at = i * 64 * kWaves + tid, t = at / LC, c = at % LC;
+  kv_u32x4 kw[NL], vw[NL];
+  float sc = 0.0f;
+  const auto load = [&](int step, int piece) {
+    const int64_t* where = lds.where[step & 7];
+    const int i = piece % NL, at = i * 64 * kWaves + tid;
+    if (piece < NL) {
+      const int t = at / LC, c = at % LC;
       kw[i] = *(const kv_u32x4*)(a.ck + where[t >> 4] + (t & 15) * row_bytes +
                                  (16 * c < row_bytes ? 16 * c : 0));
+    } else {
       const int run = at / DT, d = at % DT;
       vw[i] = *(const kv_u32x4*)(a.cv + where[run * R >> 4] + (run * R & 15) * row_bytes +
                                  16 * (d < a.c.dim ? d : 0));
     }
-    if constexpr (CODES) {
+    if (CODES && piece == 2 * NL - 1) {
       const int t = tid & (TOK - 1);
-      sc = ((tid & TOK) ? a.sv : a.sk)[lds.slot[step & 3][t >> 4] + (t & 15)];
+      sc = ((tid & TOK) ? a.sv : a.sk)[lds.slot[step & 7][t >> 4] + (t & 15)];
     }
   };
-  const auto keep = [&](int step) {
-    const int buf = step & 1;
-    const bool edge = step * TOK + TOK > hi_first || step * TOK < lo_last;
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int at = i * 64 * kWaves + tid, t = at / LC, c = at % LC;
-      const int run = at / DT, d = at % DT;
+  const auto keep = [&](int step, int piece) {
+    const int buf = step & 1, i = piece % NL, at = i * 64 * kWaves + tid;
+    if (piece < NL) {
+      const int t = at / LC, c = at % LC;
       if constexpr (CODES) {
         lds.k[buf][t * CH + 2 * c] = operand<CT>(kw[i], 0);
         lds.k[buf][t * CH + 2 * c + 1] = operand<CT>(kw[i], 1);
       } else {
         lds.k[buf][t * CH + c] = kw[i];
       }
-      // values behind some row's mask must be numbers; a token that has none
-      // counts as NaN for the rows that see it
-      if (CT != kInt8 && edge) {
-        const uint32_t bad = drop_non_finite<CT>(vw[i]);
-        if (bad) {
-          atomicOr(&lds.bad[step % 3][run * R / 8], bad & 0xFFu);
-          if (CODES) atomicOr(&lds.bad[step % 3][run * R / 8 + 1], bad >> 8);
-        }
-      }
-      if constexpr (CODES) {
-        lds.v[buf][2 * run * DT + d] = operand<CT>(vw[i], 0);
-        lds.v[buf][(2 * run + 1) * DT + d] = operand<CT>(vw[i], 1);
-      } else {
-        lds.v[buf][run * DT + d] = vw[i];
+      return;
+    }
+    const int run = at / DT, d = at % DT;
+    // values behind some row's mask must be numbers; a token that has none counts
+    // as NaN for the rows that see it
+    if (CT != kInt8 && (step * TOK + TOK > hi_first || step * TOK < lo_last)) {
+      const uint32_t bad = drop_non_finite<CT>(vw[i]);
+      if (bad) {
+        atomicOr(&lds.bad[step % 3][run * R / 8], bad & 0xFFu);
+        if (CODES) atomicOr(&lds.bad[step % 3][run * R / 8 + 1], bad >> 8);
       }
     }
     if constexpr (CODES) {
+      lds.v[buf][2 * run * DT + d] = operand<CT>(vw[i], 0);
+      lds.v[buf][(2 * run + 1) * DT + d] = operand<CT>(vw[i], 1);
+    } else {
+      lds.v[buf][run * DT + d] = vw[i];
+    }
+    if (CODES && piece == 2 * NL - 1) {
+      // a value scale that is no number counts as its value not being one
+      if (tid >= TOK && tid < 2 * TOK && !(__builtin_fabsf(sc) < __builtin_inff())) {
+        atomicOr(&lds.bad[step % 3][(tid & (TOK - 1)) >> 3], 1u << (tid & 7));
+        sc = 0.0f;
+      }
       if (tid < 2 * TOK) (tid < TOK ? lds.ks : lds.vs)[buf][tid & (TOK - 1)] = sc;
       float big = sc;                   // every TOK threads hold a whole tile's scales
 #pragma unroll
@@ -829,46 +850,57 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
       if (tid == TOK) lds.big[buf] = big;
     }
   };
+  // The pieces that belong to the k-th of n products.
+  const auto share = [](int k, int n, auto piece) {
+#pragma unroll
+    for (int i = 0; i < 2 * NL; ++i)
+      if (i * n / (2 * NL) == k) piece(i);
+  };
 
   if (step0 < step1) {
-    if (tid < TOK / 8) {
+    if (tid < 8 * G) {
       look_up(step0);
       note(step0);
-      look_up(step0 + 1);
-      note(step0 + 1);
     }
     __syncthreads();
-    load(step0);
-    keep(step0);
+    if (tid < TOK / 8) {
+      clear(step0);
+      clear(step0 + 1);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2 * NL; ++i) load(step0, i);
+#pragma unroll
+    for (int i = 0; i < 2 * NL; ++i) keep(step0, i);
     __syncthreads();
   }
+  // (the last turn fetches its own tile again: every place is clamped to those seen)
   for (int step = step0; step < step1; ++step) {
     const int buf = step & 1, t0 = step * TOK;
-    const bool more = step + 1 < step1;
-    if (more) {
-      if (tid < TOK / 8) look_up(step + 2);
-      load(step + 1);
-    }
+    const bool turn = ((step - step0) & 3) == 0 && step != step0;
+    if (turn && tid < 4 * G) look_up(step + 4);
     if (live && t0 < whi && t0 + TOK > wlo) {
+      // score e of the n-th 32 tokens: token 16 (e / 8) + 8 half + e % 8 of them.  Reads
+      // run A products ahead.
       f32x16 x[NK];
+      {
+        const int t = 16 * (col >> 4) + 8 * (col >> 2 & 1) + 4 * (col >> 3 & 1) + (col & 3);
+        const kv_u32x4* row = &lds.k[buf][t * CH + half];
+        kv_u32x4 kf[A + 1];
 #pragma unroll
-      for (int n = 0; n < NK; ++n) {
+        for (int k = 0; k < A; ++k) kf[k] = row[2 * k];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[n][e] = 0.0f;
-        const int t = 32 * n + 16 * (col >> 4) + 8 * (col >> 2 & 1) + 4 * (col >> 3 & 1) + (col & 3);
+        for (int n = 0; n < NK; ++n)
 #pragma unroll
-        for (int k = 0; k < KM; ++k)
-          x[n] = mfma32<CT>(lds.k[buf][t * CH + 2 * k + half], qf[k], x[n]);
+          for (int e = 0; e < 16; ++e) x[n][e] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NK * KM; ++k) {
+          if (k + A < NK * KM) kf[(k + A) % (A + 1)] = row[(k + A) / KM * 32 * CH + 2 * ((k + A) % KM)];
+          x[k / KM] = mfma32<CT>(kf[k % (A + 1)], qf[k % KM], x[k / KM]);
+          share(k, NK * KM, [&](int i) { load(step + 1, i); });
+          if constexpr (!CODES) __builtin_amdgcn_sched_barrier(0);
+        }
       }
-      // key reads run six ahead of the products: two waves a SIMD do not hide them all
-      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
-#pragma unroll
-      for (int i = 0; i < NK * KM - 6; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
-      // score e of tile n: token 32 n + 16 (e / 8) + 8 half + e % 8
       if constexpr (CODES)
 #pragma unroll
         for (int n = 0; n < 4 * NK; ++n) {
@@ -902,11 +934,11 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
           big = fmaxf(p.a, p.b);
         }
       }
-      float top = x[0][0];
+      float top = -__builtin_inff();
 #pragma unroll
       for (int n = 0; n < NK; ++n)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, x[n][e]);
+        for (int e = 0; e < 16; e += 2) top = max3(top, x[n][e], x[n][e + 1]);
       const Pair p = swapped<64>(top);
       const float want = base_for<CODES>(fmaxf(p.a, p.b), qs, big);
       if (__any(want > base + kSlack)) {
@@ -919,33 +951,48 @@ __global__ __launch_bounds__(64 * kWaves, DT > 128 ? 1 : 2) void tile_kernel(Att
         base = to;
       }
       const float from = base == -__builtin_inff() ? 0.0f : base;
+      // Weights of four tokens, as a half of the second product's operand.
       kv_u32x4 pw[2 * NK];
-#pragma unroll
-      for (int n = 0; n < 4 * NK; ++n) {
+      const auto weights = [&](int n) {
         f32x4 y = {1, 1, 1, 1};
         if constexpr (CODES) y = *(const f32x4*)&lds.vs[buf][16 * (n >> 1) + 8 * half + 4 * (n & 1)];
         float w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float z = x[n >> 2][4 * (n & 3) + e];
-          w[e] = __builtin_amdgcn_exp2f(fmaf(z, qs, -from));
+          w[e] = __builtin_amdgcn_exp2f(fmaf(x[n >> 2][4 * (n & 3) + e], qs, -from));
           l += w[e];
-          // (what a row does not see may have any scale)
-          if constexpr (CODES) w[e] = z == -__builtin_inff() ? 0.0f : w[e] * y[e];
+          if constexpr (CODES) w[e] *= y[e];
         }
         pw[n >> 1][2 * (n & 1)] = pack2<CT>(w[0], w[1]);
         pw[n >> 1][2 * (n & 1) + 1] = pack2<CT>(w[2], w[3]);
+      };
+      // The first sixteen tokens' weights, then each sixteen's products with the next
+      // ones' weights and the next tile's LDS writes among them.
+      constexpr int N = 2 * NK * VM;
+      const kv_u32x4* values = &lds.v[buf][half * DT + col];
+      const auto value = [&](int i) { return values[2 * (i / VM) * DT + 32 * (i % VM)]; };
+      kv_u32x4 vf[A + 1];
+#pragma unroll
+      for (int i = 0; i < A; ++i) vf[i] = value(i);
+      weights(0);
+      weights(1);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (i + A < N) vf[(i + A) % (A + 1)] = value(i + A);
+        o[i % VM] = mfma32<CT>(vf[i % (A + 1)], pw[i / VM], o[i % VM]);
+        if (i / VM + 1 < 2 * NK && i % VM % (VM / 2) == 0)
+          weights(2 * (i / VM + 1) + i % VM / (VM / 2));
+        if (i >= N / 2) share(i - N / 2, N / 2, [&](int x) { keep(step + 1, x); });
+        if constexpr (!CODES) __builtin_amdgcn_sched_barrier(0);
       }
+    } else {
 #pragma unroll
-      for (int n = 0; n < 2 * NK; ++n)
+      for (int i = 0; i < 2 * NL; ++i) load(step + 1, i);
 #pragma unroll
-        for (int v = 0; v < VM; ++v)
-          o[v] = mfma32<CT>(lds.v[buf][(2 * n + half) * DT + 32 * v + col], pw[n], o[v]);
+      for (int i = 0; i < 2 * NL; ++i) keep(step + 1, i);
     }
-    if (more) {
-      keep(step + 1);
-      if (tid < TOK / 8) note(step + 2);
-    }
+    if (turn && tid < 4 * G) note(step + 4);
+    if (tid < TOK / 8) clear(step + 2);
     __syncthreads();
   }
 
