@@ -54,7 +54,7 @@ struct AttendArgs {
   float scale;                // times log2 e, its magnitude; never 0 (2^-126 stands for it)
   uint32_t flip;              // sign bits that a negative scale puts on the queries
   // how the work is cut (see the plan)
-  int32_t block_rows, log_step, min_steps, whole_steps, units, split;
+  int32_t block_rows, log_step, min_steps, whole_few, whole_many, units, split;
   int32_t over, upto;         // sequences of over < rows <= upto are this launch's
   int32_t slices;             // workgroups that join a tile's rows
   float target;
@@ -65,8 +65,9 @@ struct AttendArgs {
 // A sequence's rows are cut in tiles of block_rows, its keys in steps of
 // 2^log_step tokens, and the steps that a sequence's rows see in equal parts, so
 // many that all parts of all sequences together come to about `target`
-// workgroups of equal work (never less than min_steps a part; one part up to
-// whole_steps).  A unit is a part
+// workgroups of equal work (never less than min_steps a part).  What a second
+// launch does not pay for stays whole: whole_few steps, or whole_many where there
+// are a quarter of `target` workgroups already.  A unit is a part
 // of a tile; units are numbered sequence by sequence, tile by tile.  Every wave
 // works the numbering out for itself, a lane a sequence.
 struct Sequence {
@@ -132,20 +133,22 @@ __device__ __forceinline__ bool find(const AttendArgs& a, Number what, int numbe
                                      int* seq, int* first_unit) {
   const int lane = threadIdx.x & 63;
   const Sequence head = sequence(a, lane);
-  int steps = 0x7fffffff;                               // of a part
+  int steps = 0x7fffffff, whole = 0x7fffffff;           // of a part, of one that stays whole
   if (a.split) {
-    float total = 0.0f;
+    float total = 0.0f, tiles = 0.0f;
     for (int b = 0; b < a.B; b += 64) {
       const Sequence s = b ? sequence(a, b + lane) : head;
       total += wave_total((float)s.tiles * (float)s.steps);
+      tiles += wave_total((float)s.tiles);
     }
     const float share = ceilf(total * (float)a.c.heads / a.target);
     steps = share > 1e9f ? 1000000000 : share > (float)a.min_steps ? (int)share : a.min_steps;
+    whole = tiles * (float)a.c.heads * 4.0f >= a.target ? a.whole_many : a.whole_few;
   }
   int before = 0, units_before = 0;
   for (int b = 0; b < a.B; b += 64) {
     Sequence s = b ? sequence(a, b + lane) : head;
-    s.parts = s.steps > a.whole_steps ? (s.steps + steps - 1) / steps : 1;
+    s.parts = s.steps > whole ? (s.steps + steps - 1) / steps : 1;
     const int units = s.tiles * s.parts, own = what == kUnitNumber ? units : s.tiles;
     const int upto = before + wave_scan(own);
     const uint64_t mask = __ballot(number >= upto - own && number < upto);
@@ -1125,11 +1128,10 @@ constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;
 constexpr int kFewRows = 32;           // rows of a sequence that stream_kernel takes
 constexpr int kTargetFew = 512, kTargetMany = 512;    // workgroups that split sequences come to
 constexpr int kMinTokens = 256;        // keys of a part of many rows, at least
-constexpr int kWholeTokens = 1024;     // keys that are not worth a second launch
 
 // One launch's share of a call: a function of sizes alone.
 struct Cut {
-  int waves, block_rows, log_step, min_steps, whole_steps, split, over, upto, target;
+  int waves, block_rows, log_step, min_steps, whole_few, whole_many, split, over, upto, target;
   int64_t tiles, units;
   size_t bytes;
 };
@@ -1144,9 +1146,14 @@ int cut(const leech_attend_args* g, const CacheShape& c, bool many, Cut* k) {
   k->log_step = many ? (c.dim > 128 ? 5 : 6) : type_bytes(c.type) == 2 ? 5 : 6;
   k->min_steps = many ? kMinTokens >> k->log_step : kStreamWaves;
   const int64_t least = (T + k->block_rows - 1) / k->block_rows;
-  k->whole_steps = kWholeTokens >> k->log_step;
-  k->split = keys > kWholeTokens && least * c.heads < k->target;
-  if (!k->split) k->whole_steps = 0x7fffffff;
+  // A round of eight waves takes about 2 us, the join 3.5: three rounds stay whole
+  // (one sequence of 700 f16 keys: 12.8 us whole, 13.0 split; of 2000 24.2 and 13.2);
+  // with the card half full already eight do (16 of 2000: 26.8 and 34.4), four where a
+  // step has twice the products (16 x 5 of 4000 int8 keys: eight 74.8, split 62.7).
+  // Many rows: up to 1024 keys.
+  k->whole_few = many ? 1024 >> k->log_step : 3 * kStreamWaves;
+  k->whole_many = many ? k->whole_few : (k->block_rows > 16 ? 4 : 8) * kStreamWaves;
+  k->split = keys > ((int64_t)k->whole_few << k->log_step) && least * c.heads < k->target;
   k->waves = many ? kWaves : kStreamWaves;
   // (two more for the roundings of the plan's f32 total)
   k->tiles = T / k->block_rows + std::min<int64_t>(g->B, g->T);
@@ -1237,7 +1244,8 @@ int launch(AttendArgs a, const Cut& k, float* workspace, hipStream_t stream) {
   a.block_rows = k.block_rows;
   a.log_step = k.log_step;
   a.min_steps = k.min_steps;
-  a.whole_steps = k.whole_steps;
+  a.whole_few = k.whole_few;
+  a.whole_many = k.whole_many;
   a.units = (int32_t)k.units;
   a.split = k.split;
   a.over = k.over;
