@@ -93,6 +93,12 @@ def parse():
     ap.add_argument("--no-step14b", action="store_true",
                     help="skip the 14B-class decode step (40 layers + fp16 head, Leech vs FP16)")
     ap.add_argument("--step14b-layers", type=int, default=40)
+    ap.add_argument("--step14b-context", type=int, default=0, metavar="TOKENS",
+                    help="also time the 14B step with what lies between q/k/v and o: rotary "
+                         "positions, the cache write and the attention over TOKENS cached tokens "
+                         "(the new one among them; 40 query and 8 cache heads of 128)")
+    ap.add_argument("--step14b-cache", default="f16", choices=("f16", "int8", "e4m3"),
+                    help="the type of that cache")
     ap.add_argument("--batch-14b", action="store_true",
                     help="also time batched launches at the 14B-class fused projection shapes")
     ap.add_argument("--sweep", action="store_true",
@@ -831,6 +837,9 @@ def bench_step14b(args, torch, P, synth):
         run_head()
 
     transcode = bench_transcode(torch, P, dcb, parts, dev)
+    attention = None
+    if args.step14b_context:
+        attention = step14b_attention(args, torch, P, fus, xs, site_inp, yf, run_head, cen)
 
     res = {}
     for name, fn in (("separate", step_sep), ("fused", step_fused), ("fused_rot", step_fused_rot),
@@ -856,7 +865,57 @@ def bench_step14b(args, torch, P, synth):
             "fp16_vs_fused_with_rotation_mixed": round(res["fp16"] / res["fused_rotmix"], 3),
             "fp16_vs_fused_with_rotation_in_kernel": round(res["fp16"] / res["fused_rotk"], 3),
             "leech_part_GBps_fused": round(L * leech_bytes / (leech_fused * 1e-6) / 1e9, 1),
+            **({"attention": attention} if attention else {}),
             "transcode": transcode}
+
+
+def step14b_attention(args, torch, P, fus, xs, site_inp, yf, run_head, cen):
+    """The fused 14B step with the operators between q/k/v and o in their place: k
+    and q turned and k, v kept (one launch), the attention of the new token over
+    the layer's own cache, its output the o product's activation."""
+    dev, n, page = torch.device("cuda:0"), args.step14b_context, 128
+    dtype = {"f16": torch.float16, "int8": torch.int8, "e4m3": torch.float8_e4m3fn}[
+        args.step14b_cache]
+    pages = -(-n // page)
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(7)
+    caches = [P.KVCache.empty(pages, page, 8, 128, dtype, dev) for _ in fus]
+    at = torch.arange(n, device=dev)
+    for c in caches:                     # numbers in every slot, so that no product is of zeros
+        for t in range(0, n, 8192):
+            kv = torch.randn(2, min(8192, n - t), 8, 128, generator=gen, device=dev)
+            c.write(kv[0], kv[1], at[t:t + 8192].contiguous())
+    turn = P.Rotary.of(128, device=dev)
+    table = torch.randperm(pages, generator=gen, device=dev).int().view(1, -1)
+    place = table[0, (n - 1) // page].long() * page + (n - 1) % page
+    slot, position = place.view(1), torch.tensor([n - 1], device=dev)
+    length = torch.tensor([n], dtype=torch.int32, device=dev)
+    heads = yf["qkv"].view(1, 56, 128)
+    q = torch.empty((1, 40, 128), dtype=torch.float16, device=dev)
+    xo = torch.zeros_like(xs[site_inp["o"].K])
+    out = xo[:5120].view(1, 40, 128)
+
+    def attend(c):
+        c.write(heads[:, 40:48], heads[:, 48:], slot, turn, position, heads[:, :40], out=q)
+        c.attend(q, table, length, out=out)
+
+    def step(_):
+        for c, layer in zip(caches, fus):
+            for f, (m, rows) in layer.items():
+                x = xo if f == "o" else xs[site_inp[f].K]
+                m.gemv_grouped(x, rows, [cen] * len(rows), yf[f])
+                if f == "qkv":
+                    attend(c)
+        run_head()
+
+    us = round(replay_us(torch, step, 3), 1)
+    alone = round(replay_us(torch, lambda i: [attend(c) for c in caches], 3), 1)
+    log(f"[bench] 14B step with attention over {n} {args.step14b_cache} tokens: {us} us, "
+        f"the operators alone {alone} us")
+    return {"context": n, "cache": args.step14b_cache, "us_fused_with_attention": us,
+            "us_write_and_attend_alone": alone,
+            "cache_bytes_read": len(caches) * n * 8 * (2 * 128 * dtype.itemsize
+                                                       + (8 if dtype.itemsize == 1 else 0))}
 
 
 BLOCKS_4B = 150_681_600     # blocks of the paper's 4B model (§3.1), for the time to unfold it
