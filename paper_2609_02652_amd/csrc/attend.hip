@@ -339,7 +339,14 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
-constexpr int kStreamWaves = 8, kWaves = 4;     // of a workgroup: stream_kernel's, the others'
+// Waves of a workgroup: stream_kernel's eight, or four where a wave needs the
+// registers of two (at dim > 128, and for 32 rows of 128 over codes, eight waves
+// spilled 100 to 300 bytes a lane: 16 sequences of 3000 int8 keys at 256 took 119 us,
+// now 48; 16 x 5 tokens of 4000 at 128 62.8, now 47), and the others' four.
+constexpr int stream_waves(bool codes, int dim, int rows) {
+  return dim > 128 || (codes && dim > 64 && rows > 16) ? 4 : 8;
+}
+constexpr int kWaves = 4;
 
 // A workgroup is a unit of up to 16·NT rows; its waves take the unit's steps in
 // turn and join at the end.  DT: the head's dimension, or the next of 64, 128,
@@ -347,16 +354,18 @@ constexpr int kStreamWaves = 8, kWaves = 4;     // of a workgroup: stream_kernel
 // are 32 registers a lane each at DT = 128, the next step's keys loading while
 // this one's weights and values are worked on and the other way round.
 template <int CT, int DT, int NT>
-__global__ __launch_bounds__(64 * kStreamWaves, DT > 128 ? 1 : 2) void stream_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * stream_waves(kBytes<CT> == 1, DT, 16 * NT),
+                             stream_waves(kBytes<CT> == 1, DT, 16 * NT) / 4) void stream_kernel(AttendArgs a) {
+  constexpr int W = stream_waves(kBytes<CT> == 1, DT, 16 * NT);
   constexpr int R = kRun<CT>, TOK = kStep<CT>, NU = R / 4;
   constexpr int KC = DT * kBytes<CT> / 64;       // sixteen-byte loads of a key row's lane
   constexpr int KM = DT / 32;                    // products along a head
   constexpr int VM = DT / 16;                    // tiles of coordinates
   constexpr int H = kBytes<CT> == 2 ? 1 : 2;     // operands in sixteen bytes
   // coordinates joined at once: a thread four of a row
-  constexpr int COLS = 4 * (64 * kStreamWaves) / (16 * NT) < DT ? 4 * (64 * kStreamWaves) / (16 * NT) : DT;
-  __shared__ float joined[kStreamWaves][16 * NT][COLS + 4];
-  __shared__ kv_f32x2 stats[16 * NT][kStreamWaves];
+  constexpr int COLS = 4 * (64 * W) / (16 * NT) < DT ? 4 * (64 * W) / (16 * NT) : DT;
+  __shared__ float joined[W][16 * NT][COLS + 4];
+  __shared__ kv_f32x2 stats[16 * NT][W];
   __shared__ float inverse[16 * NT];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int h = blockIdx.x % a.c.heads, unit = blockIdx.x / a.c.heads;
@@ -375,8 +384,8 @@ __global__ __launch_bounds__(64 * kStreamWaves, DT > 128 ? 1 : 2) void stream_ke
   int step0 = lo_first / TOK, step1 = (hi_last + TOK - 1) / TOK;
   if (step1 < step0) step1 = step0;
   // parts of whole rounds of the waves
-  const int share = ((step1 - step0 + s.parts - 1) / s.parts + kStreamWaves - 1) / kStreamWaves *
-                    kStreamWaves;
+  const int share = ((step1 - step0 + s.parts - 1) / s.parts + W - 1) / W *
+                    W;
   const int64_t from_step = step0 + (int64_t)part * share;
   step1 = from_step + share < step1 ? (int)(from_step + share) : step1;
   step0 = from_step < step1 ? (int)from_step : step1;
@@ -481,12 +490,12 @@ __global__ __launch_bounds__(64 * kStreamWaves, DT > 128 ? 1 : 2) void stream_ke
     // the pages of a step are asked for a step ahead of its keys: loads come back in
     // their order, so what waits for a page must not have asked for more before it
     const auto after = [&](int st, int n) {
-      return st + n * kStreamWaves < step1 ? st + n * kStreamWaves : st;
+      return st + n * W < step1 ? st + n * W : st;
     };
     jk = run_at(after(step, 1), col >> 2);
     jv = run_at(after(step, 1), g);
     int pk2 = page_of(jk), pv2 = page_of(jv);
-    for (;; step += kStreamWaves) {
+    for (;; step += W) {
       const bool lost = pv < 0 || pv >= a.pages;       // this lane's run has no page
       f32x4 sc[NT][NU];
 #pragma unroll
@@ -501,11 +510,11 @@ __global__ __launch_bounds__(64 * kStreamWaves, DT > 128 ? 1 : 2) void stream_ke
 #pragma unroll
           for (int t = 0; t < NT; ++t) sc[t][u] = mfma16<CT>(x, qf[t][k], sc[t][u]);
         }
-      const bool more = step + kStreamWaves < step1;
+      const bool more = step + W < step1;
       int jk3 = jk, jv3 = jv, pk3 = pk2, pv3 = pv2;
       if (more) {
-        jk3 = run_at(after(step + kStreamWaves, 1), col >> 2);
-        jv3 = run_at(after(step + kStreamWaves, 1), g);
+        jk3 = run_at(after(step + W, 1), col >> 2);
+        jv3 = run_at(after(step + W, 1), g);
         pk3 = page_of(jk3);
         pv3 = page_of(jv3);
         load_keys(pk2, jk);
@@ -610,10 +619,10 @@ __global__ __launch_bounds__(64 * kStreamWaves, DT > 128 ? 1 : 2) void stream_ke
   float f[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    kv_f32x2 y[kStreamWaves];
+    kv_f32x2 y[W];
     float top = -__builtin_inff(), sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kStreamWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       y[w] = stats[16 * t + col][w];
       top = fmaxf(top, y[w][0]);
     }
@@ -621,7 +630,7 @@ __global__ __launch_bounds__(64 * kStreamWaves, DT > 128 ? 1 : 2) void stream_ke
     f[t] = __builtin_amdgcn_exp2f(base[t] - to);
     if (wave == t && g == 0 && 16 * t + col < rows) {
 #pragma unroll
-      for (int w = 0; w < kStreamWaves; ++w) sum += y[w][1] * __builtin_amdgcn_exp2f(y[w][0] - to);
+      for (int w = 0; w < W; ++w) sum += y[w][1] * __builtin_amdgcn_exp2f(y[w][0] - to);
       const int r = 16 * t + col;
       inverse[r] = whole ? (sum != 0.0f ? 1.0f / sum : 0.0f) : 1.0f;     // a NaN sum stays one
       if (!whole)
@@ -645,7 +654,7 @@ __global__ __launch_bounds__(64 * kStreamWaves, DT > 128 ? 1 : 2) void stream_ke
     if (r >= rows || c0 + c >= a.c.dim) continue;
     f32x4 x = {0, 0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < kStreamWaves; ++w) x += *(const f32x4*)&joined[w][r][c];
+    for (int w = 0; w < W; ++w) x += *(const f32x4*)&joined[w][r][c];
     x *= inverse[r];
     if (!whole) {
       *(f32x4*)(a.part_o + (part_row + r) * a.c.dim + c0 + c) = x;
@@ -1144,17 +1153,17 @@ int cut(const leech_attend_args* g, const CacheShape& c, bool many, Cut* k) {
   const int64_t keys = (int64_t)g->table_pages << c.log_page;
   k->target = many ? kTargetMany : kTargetFew;
   k->log_step = many ? (c.dim > 128 ? 5 : 6) : type_bytes(c.type) == 2 ? 5 : 6;
-  k->min_steps = many ? kMinTokens >> k->log_step : kStreamWaves;
+  k->waves = many ? kWaves : stream_waves(type_bytes(c.type) == 1, c.dim, k->block_rows);
+  k->min_steps = many ? kMinTokens >> k->log_step : k->waves;
   const int64_t least = (T + k->block_rows - 1) / k->block_rows;
-  // A round of eight waves takes about 2 us, the join 3.5: three rounds stay whole
+  // A round of the waves takes about 2 us, the join 3.5: three rounds stay whole
   // (one sequence of 700 f16 keys: 12.8 us whole, 13.0 split; of 2000 24.2 and 13.2);
   // with the card half full already eight do (16 of 2000: 26.8 and 34.4), four where a
   // step has twice the products (16 x 5 of 4000 int8 keys: eight 74.8, split 62.7).
   // Many rows: up to 1024 keys.
-  k->whole_few = many ? 1024 >> k->log_step : 3 * kStreamWaves;
-  k->whole_many = many ? k->whole_few : (k->block_rows > 16 ? 4 : 8) * kStreamWaves;
+  k->whole_few = many ? 1024 >> k->log_step : 3 * k->waves;
+  k->whole_many = many ? k->whole_few : (k->block_rows > 16 ? 4 : 8) * k->waves;
   k->split = keys > ((int64_t)k->whole_few << k->log_step) && least * c.heads < k->target;
-  k->waves = many ? kWaves : kStreamWaves;
   // (two more for the roundings of the plan's f32 total)
   k->tiles = T / k->block_rows + std::min<int64_t>(g->B, g->T);
   k->units = k->tiles + (k->split ? (k->target + c.heads - 1) / c.heads + 2 : 0);
