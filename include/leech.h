@@ -596,7 +596,8 @@ typedef struct {
   int64_t T;               /* rows of q and out                                      */
   const void* q;           /* 16-byte aligned, strides multiples of 8 elements       */
   int64_t q_token_stride, q_head_stride;
-  void* out;               /* as q; its rows must not overlap                        */
+  void* out;               /* as q; its rows must not overlap; q itself (the same    */
+                           /* strides) or apart from it                              */
   int64_t out_token_stride, out_head_stride;
   float* lse;              /* [T][q_heads], or NULL                                  */
   int32_t B;               /* sequences                                              */

@@ -57,6 +57,7 @@ struct AttendArgs {
   int32_t block_rows, log_step, min_steps, whole_few, whole_many, units, split;
   int32_t over, upto;         // sequences of over < rows <= upto are this launch's
   int32_t slices;             // workgroups that join a tile's rows
+  int32_t direct;             // unit b is sequence b, of one tile and part
   float target;
   float *part_o, *part_ml;    // [head][unit][row][dim], [head][unit][row][2]
 };
@@ -131,6 +132,11 @@ __device__ __forceinline__ float wave_total(float v) {
 enum Number { kUnitNumber, kTileNumber };
 __device__ __forceinline__ bool find(const AttendArgs& a, Number what, int number, Sequence* out,
                                      int* seq, int* first_unit) {
+  if (a.direct) {
+    *out = sequence(a, number);
+    *seq = *first_unit = number;
+    return out->tiles > 0;
+  }
   const int lane = threadIdx.x & 63;
   const Sequence head = sequence(a, lane);
   int steps = 0x7fffffff, whole = 0x7fffffff;           // of a part, of one that stays whole
@@ -1140,7 +1146,8 @@ constexpr int kMinTokens = 256;        // keys of a part of many rows, at least
 
 // One launch's share of a call: a function of sizes alone.
 struct Cut {
-  int waves, block_rows, log_step, min_steps, whole_few, whole_many, split, over, upto, target;
+  int waves, block_rows, log_step, min_steps, whole_few, whole_many, split, direct, over, upto,
+      target;
   int64_t tiles, units;
   size_t bytes;
 };
@@ -1166,7 +1173,11 @@ int cut(const leech_attend_args* g, const CacheShape& c, bool many, Cut* k) {
   k->split = keys > ((int64_t)k->whole_few << k->log_step) && least * c.heads < k->target;
   // (two more for the roundings of the plan's f32 total)
   k->tiles = T / k->block_rows + std::min<int64_t>(g->B, g->T);
-  k->units = k->tiles + (k->split ? (k->target + c.heads - 1) / c.heads + 2 : 0);
+  // Few rows are one tile a sequence: unsplit, nothing has to be looked for (every
+  // workgroup numbering 1024 sequences would take it 20 us).
+  k->direct = !many && !k->split;
+  k->units = k->direct ? g->B
+             : k->tiles + (k->split ? (k->target + c.heads - 1) / c.heads + 2 : 0);
   if (k->units * c.heads * 64 * k->waves > kMaxThreads)
     return set_error(LEECH_E_SHAPE, "too many rows for a launch");
   k->bytes = k->split ? (size_t)(c.heads * k->units * k->block_rows) * (c.dim + 2) * sizeof(float)
@@ -1260,6 +1271,7 @@ int launch(AttendArgs a, const Cut& k, float* workspace, hipStream_t stream) {
   a.over = k.over;
   a.upto = k.upto;
   a.target = (float)k.target;
+  a.direct = k.direct;
   // a row a wave, unless that makes more workgroups than the card takes at once
   a.slices = (int32_t)std::max<int64_t>(
       1, std::min<int64_t>(k.block_rows / kWaves, 4096 / (k.tiles * a.c.heads)));

@@ -3,10 +3,11 @@ the paged key/value cache and the attention of new tokens over it (the
 `leech_rope`, `leech_cache_*` and `leech_attend` calls of include/leech.h, which
 says what each computes and how the cache lies in memory).
 
-Streams: a call runs on `stream`, or on the current one of its tensors' device;
-tensors that it allocates (results that no `out` was given for, workspaces)
-belong to the stream it runs on.  Everything on the device is asynchronous, and
-may be captured into a graph.
+Streams: a call runs on `stream`, or on the current one of its tensors' device,
+after what that stream holds already: work on other streams that its tensors wait
+for is the caller's to order.  Tensors that it allocates (results that no `out` was
+given for, workspaces) belong to the stream it runs on.  Everything on the device
+is asynchronous, and may be captured into a graph.
 """
 from __future__ import annotations
 
@@ -281,7 +282,7 @@ class KVCache:
         page_table int32 [B, table_pages]; kv_len int32 [B] counts the cached
         tokens, the new ones among them.  max_new: at least every sequence's new
         tokens (None: T).  window > 0: a query sees the last `window` keys up to its
-        own.  scale: None for dim^-1/2.  Returns out [T, q_heads, dim] of q's type
+        own.  scale: None for dim^-1/2.  `out` may be q.  Returns out [T, q_heads, dim] of q's type
         (rows of no sequence are not written), and lse f32 [T, q_heads] with
         with_lse."""
         torch = _torch()
@@ -303,6 +304,11 @@ class KVCache:
             starts = _index("q_start", q_start, torch.int32, B + 1, dev)
         elif T != B:
             raise ValueError("without q_start there is one new token a sequence")
+        most = (1 if q_start is None else T) if max_new is None else min(int(max_new), T)
+        window = int(window)
+        if most < 0 or window < 0:
+            raise ValueError("max_new and window must not be negative")
+        window = min(window, 0x7FFFFFFF)
         qs = q.stride()
         if qs[2] != 1:
             raise ValueError("q must have unit stride along a head")
@@ -318,8 +324,7 @@ class KVCache:
             args = _lib.AttendArgs(
                 kind, heads, T, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1],
                 lse.data_ptr() if with_lse else None, B, starts, lens, page_table.data_ptr(),
-                apart, width,
-                (1 if q_start is None else T) if max_new is None else max_new, int(causal), window,
+                apart, width, most, int(causal), window,
                 dim ** -0.5 if scale is None else scale, None, 0)
             size = _lib.attend_workspace(self._c, args)
             if size:

@@ -597,6 +597,68 @@ def test_a_captured_step_replays_with_new_lengths(dev):
         b.slots = saved
 
 
+@pytest.mark.parametrize("cache_type", ["bf16", "e4m3"])
+def test_a_captured_prompt_replays(dev, cache_type):
+    """Chunks of many rows (LDS above 64 KiB) and of few in one captured call, with
+    other lengths and starts on replay."""
+    b = Batch(dev, 26, [(150, 400), (2, 300), (1, 90)], 8, 2, 128, 32, "bf16", cache_type)
+    out = torch.zeros_like(b.q)
+    b.attend(out=out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        b.attend(out=out)
+    for lens in ([(150, 400), (2, 300), (1, 90)], [(1, 399), (100, 200), (52, 90)],
+                 [(0, 17), (0, 0), (153, 90)]):
+        starts = np.concatenate([[0], np.cumsum([n for n, _ in lens])])
+        b.q_start.copy_(torch.from_numpy(starts.astype(np.int32)))
+        b.kv_len.copy_(torch.tensor([n for _, n in lens], dtype=torch.int32))
+        out.fill_(5.0)
+        g.replay()
+        torch.cuda.synchronize()
+        eager = torch.full_like(out, 5.0)
+        b.attend(out=eager)
+        torch.cuda.synchronize()
+        assert (out == eager).all()
+        # max_new (150) leaves the rows past it alone
+        b.lens, b.starts = [(min(n, 150), length) for n, length in lens], starts
+        if max(n for n, _ in lens) <= 150:
+            saved = b.slots
+            b.slots = [s[:length] for s, (_, length) in zip(b.slots, lens)]
+            b.check(out)
+            b.slots = saved
+        else:
+            assert (out[150:] == 5).all() and torch.isfinite(out[:150].float()).all()
+
+
+@pytest.mark.parametrize("B,q_heads,heads", [(70, 2, 1), (130, 3, 3), (300, 8, 4)])
+def test_many_sequences(dev, B, q_heads, heads):
+    """More sequences than a wave has lanes: split (few workgroups) and not."""
+    rng = np.random.default_rng(B)
+    long = 3000 if heads == 1 else 500
+    lens = [(int(rng.integers(0, 3)), int(rng.integers(0, 60))) for _ in range(B)]
+    lens[3], lens[B - 2] = (1, long), (2, long - 7)
+    b = Batch(dev, 27, lens, q_heads, heads, 64, 16, "f16", "f16")
+    out, lse = b.attend(with_lse=True)
+    torch.cuda.synchronize()
+    b.check(out, lse)
+    ones = [i for i, (n, _) in enumerate(lens) if n == 1]
+    q = b.q[torch.from_numpy(b.starts[ones]).to(dev)]
+    at = torch.tensor(ones).to(dev)
+    got = b.cache.attend(q, b.table[at], b.kv_len[at])
+    want = f64(out)[b.starts[ones]]
+    # (another split: both are within the tolerance of the oracle)
+    assert np.abs(f64(got) - want).max() <= 2.0 ** -8
+
+
+def test_out_may_be_the_queries(dev):
+    for lens, heads in (([(1, 3000), (3, 70)], 4), ([(90, 200), (40, 40)], 8)):
+        b = Batch(dev, 28, lens, heads, 2, 64, 16, "f16", "int8")
+        want = b.attend()
+        assert b.attend(out=b.q) is b.q
+        assert (b.q == want).all()
+
+
 def test_two_streams_at_once(dev):
     """Calls on two streams share nothing: each allocates its own workspace."""
     one = Batch(dev, 23, [(1, 9000), (1, 3000)], 8, 1, 128, 64, "f16", "f16")
