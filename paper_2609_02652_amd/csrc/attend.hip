@@ -1173,8 +1173,8 @@ int cut(const leech_attend_args* g, const CacheShape& c, bool many, Cut* k) {
   k->split = keys > ((int64_t)k->whole_few << k->log_step) && least * c.heads < k->target;
   // (two more for the roundings of the plan's f32 total)
   k->tiles = T / k->block_rows + std::min<int64_t>(g->B, g->T);
-  // Few rows are one tile a sequence: unsplit, nothing has to be looked for (every
-  // workgroup numbering 1024 sequences would take it 20 us).
+  // Few rows are one tile a sequence: unsplit, nothing has to be looked for
+  // (1024 sequences of 300 f16 keys: 603 us when every workgroup numbers them, 326).
   k->direct = !many && !k->split;
   k->units = k->direct ? g->B
              : k->tiles + (k->split ? (k->target + c.heads - 1) / c.heads + 2 : 0);
