@@ -561,8 +561,8 @@ int leech_cache_write(const leech_kv_cache* cache, int64_t T, const leech_rows* 
                       const leech_rotary* rotary, int32_t q_heads, const leech_rows* q,
                       const leech_rows* q_out, void* stream);
 
-/* Read T slots back as rows of f32, f16 or bf16 (code · scale, rounded once);
- * a slot below 0 or past the cache reads as zeros.  Slots may repeat.
+/* Read T slots back as rows of f32, f16 or bf16, both of one type (code · scale,
+ * rounded once); a slot below 0 or past the cache reads as zeros.  Slots may repeat.
  * Asynchronous on `stream`. */
 int leech_cache_read(const leech_kv_cache* cache, int64_t T, const int64_t* d_slots,
                      const leech_rows* k_out, const leech_rows* v_out, void* stream);

@@ -105,7 +105,8 @@ def test_cache_write_refuses(args, code):
     ((cache(), -1, FAKE, rows(), rows()), SHAPE), ((cache(), 4, None, rows(), rows()), ARG),
     ((cache(), 4, FAKE, rows(0), rows()), ARG), ((cache(), 4, FAKE, rows(), None), ARG),
     ((cache(), 4, FAKE, rows(), rows(token=64)), SHAPE),
-    ((cache(), 4, FAKE, rows(type=_lib.E4M3), rows()), ARG)])
+    ((cache(), 4, FAKE, rows(type=_lib.E4M3), rows()), ARG),
+    ((cache(), 4, FAKE, rows(type=_lib.BF16), rows()), ARG)])
 def test_cache_read_refuses(args, code):
     refused(code, _lib.cache_read, *args)
 
