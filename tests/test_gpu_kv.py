@@ -504,6 +504,60 @@ def test_bad_pages_lengths_and_starts_stay_in_bounds(dev):
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("cache_type", ["bf16", "e4m3"])
+def test_bad_pages_of_a_chunk(dev, cache_type):
+    """Many rows: only those that see a place of the missing page become NaN."""
+    b = Batch(dev, 30, [(80, 200), (70, 180)], 4, 2, 64, 16, "bf16", cache_type)
+    good = f64(b.attend())
+    b.table[0, 9] = b.cache.pages                # places 144..159: position 144 is row 24
+    out = f64(b.attend())
+    assert (out[:24] == good[:24]).all() and (out[80:] == good[80:]).all()
+    assert np.isnan(out[24:80]).all()
+    out = f64(b.attend(window=30))               # rows from position 189 on do not see 159
+    assert np.isnan(out[24:69]).all() and np.isfinite(out[69:]).all()
+
+
+@pytest.mark.parametrize("new", [2, 60])
+def test_scales_and_codes_that_are_no_numbers(dev, new):
+    """In the cache itself: a NaN code, an infinite or NaN scale of a key or a value."""
+    length = 100
+    for kind in ("int8", "e4m3"):
+        b = Batch(dev, 31, [(new, length), (1, 30)], 4, 2, 64, 16, "f16", kind)
+        clean = f64(b.attend())
+        slot = int(b.slots[0][length - 1])       # the last token: seen by the last row
+        page, place = slot // 16, slot % 16
+        for part, bad in (("k_scale", math.nan), ("v_scale", math.nan), ("v_scale", math.inf),
+                          ("k", None), ("v", None)):
+            if bad is None and kind == "int8":
+                continue
+            t = getattr(b.cache, part)
+            saved = t.clone() if bad is not None else bits(t).clone()
+            if bad is not None:
+                t[page, 0, place] = bad
+            elif part == "k":
+                bits(t)[page, 0, place, 7] = 0x7F
+            else:
+                bits(t)[page, 0, 0, 7, place] = 0xFF
+            out = f64(b.attend())
+            assert (out[:new - 1] == clean[:new - 1]).all(), (kind, part, bad)
+            assert (out[new:] == clean[new:]).all() and (out[:, 2:] == clean[:, 2:]).all()
+            assert (~np.isfinite(out[new - 1, :2])).any(-1).all(), (kind, part, bad)
+            if bad is not None:
+                t.copy_(saved)
+            else:
+                bits(t).copy_(saved)
+
+
+@pytest.mark.parametrize("q_type,cache_type", [("f16", "f16"), ("bf16", "int8"), ("f16", "e4m3")])
+@pytest.mark.parametrize("dim,window", [(64, 0), (128, 700), (192, 0)])
+def test_chunks_over_long_contexts_split(dev, dim, window, q_type, cache_type):
+    """Many rows whose keys are split over workgroups and joined."""
+    b = Batch(dev, 32, [(41, 2500), (9, 1300), (33, 3001)], 4, 1, dim, 32, q_type, cache_type)
+    out, lse = b.attend(window=window, with_lse=True)
+    torch.cuda.synchronize()
+    b.check(out, lse, window=window)
+
+
 def test_rows_of_no_sequence_are_left_alone(dev):
     for lens, q_heads in (([(2, 40), (1, 9)], 4), ([(60, 80), (30, 30)], 8)):
         b = Batch(dev, 18, lens, q_heads, 2, 64, 16, "f16", "f16")
