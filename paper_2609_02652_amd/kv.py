@@ -18,36 +18,25 @@ import numpy as np
 
 from . import _lib
 
-
-def _torch():
+try:
     import torch
-    return torch
-
-
-_TYPES = {}
-
-
-def _types():
-    """torch type -> the library's."""
-    if not _TYPES:
-        torch = _torch()
-        _TYPES.update({torch.float32: _lib.F32, torch.float16: _lib.F16,
-                       torch.bfloat16: _lib.BF16, torch.int8: _lib.INT8,
-                       torch.float8_e4m3fn: _lib.E4M3})
-    return _TYPES
-
-
+except ImportError:          # the host half of the library needs none
+    torch = None
+else:
+    # torch type -> the library's
+    _TYPES = {torch.float32: _lib.F32, torch.float16: _lib.F16, torch.bfloat16: _lib.BF16,
+              torch.int8: _lib.INT8, torch.float8_e4m3fn: _lib.E4M3}
 _HERE = nullcontext()
 
 
 def _on(device, stream):
     """(context to run a call in, its stream's handle)."""
-    torch = _torch()
     if stream is None:
-        handle = torch._C._cuda_getCurrentRawStream(device.index)
+        index = device.index
+        handle = torch._C._cuda_getCurrentRawStream(index)
         # (cheaper than torch.cuda.current_device(), which sees to the set-up that a
         # GPU tensor has had)
-        if device.index == torch._C._cuda_getDevice():
+        if index == torch._C._cuda_getDevice():
             return _HERE, handle
         return torch.cuda.device(device), handle
     if not hasattr(stream, "cuda_stream"):
@@ -60,6 +49,13 @@ def _on(device, stream):
     return torch.cuda.stream(stream), stream.cuda_stream
 
 
+def _new(like, dtype):
+    """A contiguous tensor of like's shape and device."""
+    if like.is_contiguous():         # half a microsecond less than by shape
+        return torch.empty_like(like) if like.dtype == dtype else torch.empty_like(like, dtype=dtype)
+    return torch.empty(like.shape, dtype=dtype, device=like.device)
+
+
 def _gpu(name, t, device=None):
     if not t.is_cuda or (device is not None and t.device != device):
         raise ValueError(f"{name} must be on {device or 'a GPU'}, not on {t.device}")
@@ -67,7 +63,7 @@ def _gpu(name, t, device=None):
 
 def _rows(name, x, shape, device):
     """leech_rows of a tensor `shape` = (T, heads, dim) with unit stride along a head."""
-    kind = _types().get(x.dtype)
+    kind = _TYPES.get(x.dtype)
     if kind is None or kind > _lib.BF16 or x.shape != shape:
         raise ValueError(f"{name} must be an f32, f16 or bf16 tensor {list(shape)}, "
                          f"not {x.dtype} {list(x.shape)}")
@@ -80,7 +76,8 @@ def _rows(name, x, shape, device):
 
 
 def _index(name, t, dtype, n, device):
-    if t.dtype != dtype or t.shape != (n,) or not t.is_contiguous() or t.device != device:
+    if (t.dtype != dtype or t.dim() != 1 or t.numel() != n or not t.is_contiguous()
+            or t.device != device):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} entries on {device}")
     return t.data_ptr()
 
@@ -124,7 +121,6 @@ class Rotary:
     width / 2), or (2i, 2i + 1) when interleaved."""
 
     def __init__(self, freq, interleaved=False, magnitude=1.0):
-        torch = _torch()
         if freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_contiguous():
             raise ValueError("freq must be a contiguous 1-D f64 tensor")
         self.freq, self.interleaved, self.magnitude = freq, bool(interleaved), float(magnitude)
@@ -136,14 +132,13 @@ class Rotary:
     def of(cls, width, interleaved=False, device="cuda", **how):
         """From rotary_frequencies(width, **how)."""
         freq, magnitude = rotary_frequencies(width, **how)
-        return cls(_torch().from_numpy(freq).to(device), interleaved, magnitude)
+        return cls(torch.from_numpy(freq).to(device), interleaved, magnitude)
 
 
 def rope(x, positions, rotary: Rotary, out=None, dtype=None, transpose=False, stream=None):
     """x [T, heads, dim] (f32, f16 or bf16, any token and head strides) turned by
     positions int64 [T] -> a tensor of `dtype` (x's if None), or `out`, which may
     be x.  transpose: by the opposite angles (the gradient's pass)."""
-    torch = _torch()
     if x.dim() != 3:
         raise ValueError("x must be a tensor [T, heads, dim]")
     _gpu("x", x)
@@ -158,7 +153,7 @@ def rope(x, positions, rotary: Rotary, out=None, dtype=None, transpose=False, st
     ctx, handle = _on(dev, stream)
     with ctx:
         if out is None:
-            out = torch.empty(shape, dtype=dtype or x.dtype, device=dev)
+            out = _new(x, dtype or x.dtype)
         _lib.rope(T, heads, dim, cx, pos, rotary._c, transpose, _rows("out", out, shape, dev),
                   handle)
     return out
@@ -172,8 +167,7 @@ class KVCache:
     the 8-bit ones f32 scales [pages, heads, page_size] of each."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
-        torch = _torch()
-        kind = _types().get(k.dtype)
+        kind = _TYPES.get(k.dtype)
         if kind not in (_lib.F16, _lib.BF16, _lib.INT8, _lib.E4M3) or k.dim() != 4:
             raise ValueError("k must be an f16, bf16, int8 or float8_e4m3fn tensor "
                              "[pages, heads, page_size, dim]")
@@ -203,7 +197,6 @@ class KVCache:
     @classmethod
     def empty(cls, pages, page_size, heads, dim, dtype, device="cuda"):
         """A cache of zeros."""
-        torch = _torch()
         if dtype not in (torch.float16, torch.bfloat16, torch.int8, torch.float8_e4m3fn):
             raise ValueError("a cache is f16, bf16, int8 or float8_e4m3fn")
         run = 16 // dtype.itemsize
@@ -222,7 +215,6 @@ class KVCache:
         not kept), k turned by positions int64 [T] first if a rotary is given.
         With q [T, q_heads, dim], the same launch turns q into `out` (or a new
         tensor of `dtype`, q's if None) and returns it."""
-        torch = _torch()
         T, dev = k.shape[0], self.device
         shape = (T, self.heads, self.dim)
         ck, cv = _rows("k", k, shape, dev), _rows("v", v, shape, dev)
@@ -250,7 +242,7 @@ class KVCache:
         ctx, handle = _on(dev, stream)
         with ctx:
             if q is not None and out is None:
-                out = torch.empty(q_shape, dtype=dtype or q.dtype, device=dev)
+                out = _new(q, dtype or q.dtype)
             _lib.cache_write(self._c, T, ck, cv, at, pos, turn, q_heads, cq,
                              None if q is None else _rows("out", out, q_shape, dev), handle)
         return out
@@ -258,7 +250,6 @@ class KVCache:
     def read(self, slots, dtype=None, out=None, stream=None):
         """(k, v) [T, heads, dim] of slots int64 [T] as `dtype` (f16 if None), or
         in the pair `out`; a slot out of range reads as zeros."""
-        torch = _torch()
         T = slots.numel()
         at = _index("slots", slots, torch.int64, T, self.device)
         shape = (T, self.heads, self.dim)
@@ -285,8 +276,7 @@ class KVCache:
         own.  scale: None for dim^-1/2.  `out` may be q.  Returns out [T, q_heads, dim] of q's type
         (rows of no sequence are not written), and lse f32 [T, q_heads] with
         with_lse."""
-        torch = _torch()
-        kind = _types().get(q.dtype)
+        kind = _TYPES.get(q.dtype)
         if kind not in (_lib.F16, _lib.BF16) or q.dim() != 3 or q.shape[2] != self.dim:
             raise ValueError(f"q must be an f16 or bf16 tensor [T, q_heads, {self.dim}]")
         dev = self.device
@@ -318,7 +308,7 @@ class KVCache:
         ctx, handle = _on(dev, stream)
         with ctx:
             if out is None:
-                out = torch.empty((T, heads, dim), dtype=q.dtype, device=dev)
+                out = _new(q, q.dtype)
             os_ = out.stride()
             lse = torch.empty((T, heads), dtype=torch.float32, device=dev) if with_lse else None
             args = _lib.AttendArgs(
