@@ -1,0 +1,76 @@
+"""The attention's numbers where they are hardest, against f64 from the oracle.
+
+u is a type's half step (f16 2^-11, bf16 2^-8); tolerances are derived at each test.
+"""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2609_02652_amd as P  # noqa: E402
+from oracle import kv as O  # noqa: E402
+from test_gpu_kv import TYPES, U, f64, numbers, say  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU visible")
+    return torch.device("cuda:0")
+
+
+def light_keys_beside_a_heavy_one(dev, B, new, spread, q_type, cache_type):
+    """32845 keys that share a thousandth of a row's mass, beside one that has the
+    rest and a value of 0: out is the light ones' alone.  Neither call's keys are
+    split over workgroups (512 of them either way): one base and sum for a tile of
+    rows, one for each wave of a single token.  Yields for three rows (of a
+    group's heads each) out, lse, the oracle's out, lse and weights, a bound of a
+    score's error, and the values."""
+    n, heads, group, dim, page = 32845, 8, 8, 64, 64
+    say(f"[attend] heavy key: B={B} new={new} spread={spread} {q_type} over {cache_type}")
+    rng = np.random.default_rng(3)
+    pages = -(-n // page)
+    cache = P.KVCache.empty(pages, page, heads, dim, TYPES[cache_type], dev)
+    heavy, mass = 12_345, 0.999
+    k = spread * numbers(rng, (n, heads, dim), "f32")
+    k[..., 0] = 0
+    k[heavy] = 0
+    k[heavy, :, 0] = math.log(mass / (1 - mass) * n) + 0.5 * spread ** 2
+    v = 1 + 0.2 * numbers(rng, (n, heads, dim), "f32").clamp(-4.5, 4.5)
+    v[heavy] = 0
+    slots = torch.from_numpy(rng.permutation(pages)[np.arange(n) // page] * page
+                             + np.arange(n) % page).to(dev)
+    cache.write(k.to(dev), v.to(dev), slots)
+    table = (slots[::page] // page).int().expand(B, -1).contiguous()
+    q = numbers(rng, (B * new, heads * group, dim), "f32")
+    q[..., 0] = 8.0                              # scale · 8 · k[0] = k[0]
+    q = q.to(TYPES[q_type]).to(dev)
+    starts = torch.arange(B + 1, dtype=torch.int32, device=dev) * new
+    out, lse = cache.attend(q, table, torch.full((B,), n, dtype=torch.int32, device=dev), starts,
+                            max_new=new, causal=False, with_lse=True)
+    k64, v64 = (f64(t) for t in cache.read(slots, dtype=torch.float32))
+    for row, head in ((0, 0), (B * new // 2 + 5, 3), (B * new - 1, heads - 1)):
+        own = slice(head * group, (head + 1) * group)
+        q64, kh, vh = f64(q[row:row + 1, own]), k64[:, head:head + 1], v64[:, head:head + 1]
+        want, want_lse, w = O.attend64(q64, kh, vh, 1, n, causal=False)
+        es = (dim + 8) * 2.0 ** -24 / 8 * (np.abs(q64[0]) @ np.abs(kh[:, 0]).T).max(1) + 2.0 ** -21
+        yield f64(out[row, own]), f64(lse[row, own]), want[0], want_lse[0], w[0], es, vh[:, 0]
+
+
+HEAVY = [(B, new, spread) + pair for B, new in ((64, 1), (1, 1024)) for spread in (0.0, 1.0)
+         for pair in (("f16", "f16"), ("f16", "int8"), ("bf16", "e4m3"), ("bf16", "bf16"))]
+
+
+@pytest.mark.parametrize("case", HEAVY)
+def test_the_sum_of_light_weights_beside_a_heavy_one(dev, case):
+    """The sum of the weights takes a step's (of 32 tokens at least) as one f32
+    addition, and a step's are 64 at most: a relative error of (n / 32 + 64) 2^-24."""
+    for _, lse, _, want, w, es, _ in light_keys_beside_a_heavy_one(dev, *case):
+        bound = es + (w.shape[1] / 32 + 64) * 2.0 ** -24 + 2.0 ** -21 * (1 + want)
+        far = np.abs(lse - want) / bound
+        say(f"    lse {want[0]:.3f}, error {np.abs(lse - want).max():.2e}, of the bound {far.max():.2f}")
+        assert (far <= 1).all()
