@@ -580,7 +580,11 @@ int leech_cache_read(const leech_kv_cache* cache, int64_t T, const int64_t* d_sl
  * Products are on the matrix cores with f32 sums, in the type of a 16-bit cache;
  * over an 8-bit one in f16, which holds every code (bf16 queries enter it times
  * a power of two a row).  Maxima, sums and scales are f32; the weights
- * e^(s_j − m) are rounded to the products' type for the second one.  Rows of q and out before q_start[0] or from
+ * e^(s_j − m) are rounded to the products' type for the second one: by up to
+ * 2^-8 of themselves in bf16; in f16 by up to 2^-11 of themselves, or 2^-36 of
+ * the row's largest so far (over an 8-bit cache: weights times their values' scales,
+ * against the largest weight times the largest scale).  Scores are f32: those that
+ * are larger than 2^26 in magnitude are too coarse for a result.  Rows of q and out before q_start[0] or from
  * q_start[B] on are not read or written.  Lengths, starts and pages are read on
  * the device; what lies out of range there stays in bounds: starts are clamped
  * to [0, T], L_b to [0, table_pages · page_size], and a page that is not in

@@ -74,3 +74,58 @@ def test_the_sum_of_light_weights_beside_a_heavy_one(dev, case):
         far = np.abs(lse - want) / bound
         say(f"    lse {want[0]:.3f}, error {np.abs(lse - want).max():.2e}, of the bound {far.max():.2f}")
         assert (far <= 1).all()
+
+
+@pytest.mark.parametrize("case", HEAVY)
+def test_light_keys_beside_a_heavy_one(dev, case):
+    """A weight times its value's scale, over the largest weight and the largest scale
+    (equal to a few bits here: values are 0, or between 0.1 and 1.9), is off by u of
+    itself or 2^-36.  The sum's error as above, a score's e_s twice (above and below
+    the fraction), out's own rounding; what f16 holds under 2^-14 is off by 2^-25."""
+    q_type, cache_type = case[-2:]
+    for out, _, want, _, w, es, v in light_keys_beside_a_heavy_one(dev, *case):
+        n, av = w.shape[1], w @ np.abs(v)
+        u = U["bf16" if cache_type == "bf16" else "f16"]       # the second product's type
+        bound = ((u + 2 * es + (n / 32 + 64) * 2.0 ** -24)[:, None] * av + U[q_type] * np.abs(want)
+                 + 2.0 ** -25)
+        if cache_type != "bf16":
+            bound += n * 2.0 ** -36 * w.max(1)[:, None] * np.abs(v).max()
+        far = np.abs(out - want) / bound
+        say(f"    out {np.abs(want).mean():.2e}, error {np.abs(out - want).max():.2e}, "
+            f"of the bound {far.max():.2f}")
+        assert (far <= 1).all()
+
+
+@pytest.mark.parametrize("size", [2.0 ** 10, 2.0 ** 20, 2.0 ** 25])
+@pytest.mark.parametrize("q_type,cache_type", [("f16", "f16"), ("bf16", "int8"), ("bf16", "bf16")])
+@pytest.mark.parametrize("new", [1, 70])
+def test_scores_of_any_size(dev, new, size, q_type, cache_type):
+    """Scores that grow along the keys up to `size` (512 steps; in bf16 and int8 some
+    neighbours are equal).  Equal scores weigh alike, whatever their size; a distance
+    between others is off by twice e_s = 2^-22 size (the product, its scale, the base)."""
+    n, dim = 512, 64
+    k = torch.zeros(n, 1, dim)
+    k[:, 0, 0] = torch.arange(n) / n                          # exact in f16, a code's multiple
+    k[:, 0, 1] = 1.0                                          # int8: a scale of 1 / 127
+    v = numbers(np.random.default_rng(4), (n, 1, dim), "f32")
+    cache = P.KVCache.empty(n // 16, 16, 1, dim, TYPES[cache_type], dev)
+    slots = torch.arange(n).to(dev)
+    cache.write(k.to(dev), v.to(dev), slots)
+    table = torch.arange(n // 16, dtype=torch.int32, device=dev).view(1, -1)
+    q = torch.zeros(new, 1, dim)
+    q[:, 0, 0] = 128.0
+    q = q.to(TYPES[q_type]).to(dev)
+    starts = torch.tensor([0, new], dtype=torch.int32, device=dev)
+    out, lse = cache.attend(q, table, torch.tensor([n], dtype=torch.int32, device=dev), starts,
+                            scale=size / 128, with_lse=True)
+    k64, v64 = (f64(t) for t in cache.read(slots, dtype=torch.float32))
+    want, want_lse, w = O.attend64(f64(q), k64, v64, new, n, scale=size / 128)
+    es = 2.0 ** -22 * size
+    av = w[:, 0] @ np.abs(v64[:, 0])
+    bound = (U[q_type] + U["bf16" if cache_type == "bf16" else "f16"]) * av + 2.0 ** -20
+    top = w[:, 0] == w[:, 0].max(-1, keepdims=True)
+    mixed = (w[:, 0] * ~top).sum(-1)[:, None]              # mass of scores under the largest
+    bound += np.where(mixed > 2.0 ** -30, 2 * math.expm1(min(2 * es, 1.0)), 0.0) * av
+    err = np.abs(f64(out)[:, 0] - want[:, 0])
+    assert (err <= bound).all(), float((err - bound).max())
+    assert (np.abs(f64(lse) - want_lse) <= 2 * es + 2.0 ** -20).all()
