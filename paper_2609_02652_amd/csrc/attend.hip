@@ -360,12 +360,10 @@ __device__ __forceinline__ float moved_base(float base, float top, float qs, flo
   return outgrown<CT>(base, top, qs, lift) ? fmaf(top, qs, lift - kLift<CT>) : base;
 }
 
-// Largest of three, numbers before NaN.  (fmaxf first makes every operand canonical,
-// an instruction each: what the products return already is.)
+// Largest of three, numbers before NaN: one instruction, and the compiler keeps the
+// wait behind a matrix product (it does not for an instruction in inline assembly).
 __device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
-  return d;
+  return fmaxf(fmaxf(a, b), c);
 }
 
 // Waves of a workgroup: stream_kernel's eight, or four where a wave needs the
