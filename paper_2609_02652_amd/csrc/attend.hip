@@ -1135,11 +1135,11 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(AttendArgs a) {
           y[u] = *(const f32x4*)(a.part_o + (at + (int64_t)(p0 + k) * a.block_rows) * a.c.dim +
                                  (in ? c : 0));
           w[u] = __shfl(f, k, 64);
-          w[u] = i < n ? w[u] : 0.0f;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (w[u] != 0.0f) x += y[u] * w[u];          // (a part that saw nothing may hold anything)
+          // (a weight of 0 too: what is no number in a part reaches the row)
+          if (p + u * team * each + sub < n) x += y[u] * w[u];
       }
     }
 #pragma unroll

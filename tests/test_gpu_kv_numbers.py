@@ -129,3 +129,32 @@ def test_scores_of_any_size(dev, new, size, q_type, cache_type):
     err = np.abs(f64(out)[:, 0] - want[:, 0])
     assert (err <= bound).all(), float((err - bound).max())
     assert (np.abs(f64(lse) - want_lse) <= 2 * es + 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("cache_type", ["f16", "int8", "e4m3"])
+@pytest.mark.parametrize("new", [1, 40])
+def test_a_value_that_is_no_number_in_a_part_of_no_weight(dev, new, cache_type):
+    """Keys split over workgroups; the part with the NaN has weights of e^-400 beside
+    the others': 0 in f32, and still its rows are not finite."""
+    n, dim = 9000, 64
+    rng = np.random.default_rng(5)
+    k = numbers(rng, (n, 1, dim), "f32")
+    k[..., 0] = 0
+    k[:4000, :, 0] = -400.0
+    v = numbers(rng, (n, 1, dim), "f32")
+    q = numbers(rng, (2 * new, 1, dim), "f16").to(dev)
+    q[..., 0] = 8.0
+    cache = P.KVCache.empty(2 * (n // 16 + 1), 16, 1, dim, TYPES[cache_type], dev)
+    table = torch.arange(cache.pages, dtype=torch.int32, device=dev).view(2, -1)
+    lens = torch.tensor([n, n], dtype=torch.int32, device=dev)
+    starts = torch.tensor([0, new, 2 * new], dtype=torch.int32, device=dev)
+    at = torch.arange(n).to(dev)
+    for first in (0, cache.pages // 2 * 16):
+        cache.write(k.to(dev), v.to(dev), at + first)
+    clean = cache.attend(q, table, lens, starts, max_new=new)
+    assert torch.isfinite(clean).all()
+    v[1000, 0, 7] = math.nan
+    cache.write(k[1000:1001].to(dev), v[1000:1001].to(dev), at[1000:1001])
+    out = cache.attend(q, table, lens, starts, max_new=new)
+    assert torch.isnan(out[:new, 0, 7]).all()
+    assert (out[new:] == clean[new:]).all()
