@@ -327,7 +327,7 @@ __device__ __forceinline__ float to_f16(kv_u32x4* q, float scale) {
       const uint32_t w = q[m][e];
       q[m][e] = pack2<kF16>(ldexpf(bf16_value(w & 0xFFFFu), -ex), ldexpf(bf16_value(w >> 16), -ex));
     }
-  return fmaxf(ldexpf(scale, ex), 0x1p-126f);
+  return fminf(fmaxf(ldexpf(scale, ex), 0x1p-126f), __FLT_MAX__);
 }
 
 // How far the largest score seen lies above a row's base: with products in f16 up to
@@ -1395,7 +1395,8 @@ extern "C" int leech_attend(const leech_kv_cache* cache, const leech_attend_args
   a.max_new = g->max_new;
   a.causal = g->causal;
   a.window = g->window;
-  a.scale = std::max(std::fabs(g->scale) * kLog2e, 0x1p-126f);
+  // (an infinite one would make NaN of a product that is 0)
+  a.scale = std::min(std::max(std::fabs(g->scale) * kLog2e, 0x1p-126f), __FLT_MAX__);
   a.flip = g->scale < 0.0f ? 0x80008000u : 0u;
   float* room = (float*)g->workspace;
   if (k.few.units && (rc = launch(a, k.few, room, (hipStream_t)stream))) return rc;

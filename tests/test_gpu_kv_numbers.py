@@ -158,3 +158,27 @@ def test_a_value_that_is_no_number_in_a_part_of_no_weight(dev, new, cache_type):
     out = cache.attend(q, table, lens, starts, max_new=new)
     assert torch.isnan(out[:new, 0, 7]).all()
     assert (out[new:] == clean[new:]).all()
+
+
+@pytest.mark.parametrize("q_type,cache_type,size,scale", [("f16", "f16", 1.0, 3e38),
+                                                          ("bf16", "bf16", 1.0, -3e38),
+                                                          ("bf16", "int8", 2.0 ** 100, 2.0 ** 60)])
+@pytest.mark.parametrize("new", [1, 40])
+def test_scales_at_the_end_of_their_range(dev, new, q_type, cache_type, size, scale):
+    """Keys of zeros: every score is 0 whatever the scale (times log2 e, or times the
+    power of two taken out of a bf16 query, it would pass f32's range)."""
+    n, dim = 100, 64
+    v = numbers(np.random.default_rng(6), (n, 1, dim), "f32").to(dev)
+    cache = P.KVCache.empty(7, 16, 1, dim, TYPES[cache_type], dev)
+    slots = torch.arange(n).to(dev)
+    cache.write(torch.zeros_like(v), v, slots)
+    table = torch.arange(7, dtype=torch.int32, device=dev).view(1, -1)
+    q = torch.full((new, 1, dim), size, dtype=TYPES[q_type], device=dev)
+    out, lse = cache.attend(q, table, torch.tensor([n], dtype=torch.int32, device=dev),
+                            torch.tensor([0, new], dtype=torch.int32, device=dev), causal=False,
+                            scale=scale, with_lse=True)
+    v64 = f64(cache.read(slots, dtype=torch.float32)[1])[:, 0]
+    # weights are equal (over int8 rounded with their values' scales: u each)
+    bound = 2 * U[q_type] * np.abs(v64).mean(0) + 2.0 ** -20
+    assert (np.abs(f64(out)[:, 0] - v64.mean(0)) <= bound).all()
+    assert (np.abs(f64(lse) - math.log(n)) <= 2.0 ** -18).all()
