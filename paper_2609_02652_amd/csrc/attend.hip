@@ -1253,7 +1253,7 @@ int check_sizes(const leech_kv_cache* cache, const leech_attend_args* g, CacheSh
     return set_error(LEECH_E_ARG, "a 16-bit cache must have the queries' type");
   if (g->q_heads <= 0 || g->q_heads > 65535 || g->q_heads % cache->heads)
     return set_error(LEECH_E_SHAPE, "query heads must be a multiple of the cache's, up to 65535");
-  if (g->T < 0 || g->B < 0 || g->max_new < 0 || g->T * g->q_heads > 0x7fffffff)
+  if (g->T < 0 || g->B < 0 || g->max_new < 0 || g->T > 0x7fffffff / g->q_heads)
     return set_error(LEECH_E_SHAPE, "B and max_new must not be negative, T · q_heads 0 to 2^31 - 1");
   if (g->table_pages < 0 || ((int64_t)g->table_pages << shape->log_page) > 0x7fffff00)
     return set_error(LEECH_E_SHAPE, "a row of the page table holds fewer than 2^31 - 256 tokens");

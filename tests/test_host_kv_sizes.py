@@ -1,0 +1,15 @@
+"""Sizes of the attention whose products pass 64 bits: refused on the host (stand-in
+device pointers are never dereferenced)."""
+import pytest
+
+pytest.importorskip("torch")
+
+from paper_2609_02652_amd import _lib  # noqa: E402
+from test_host_kv import SHAPE, attend_args, cache, refused  # noqa: E402
+
+
+@pytest.mark.parametrize("T,q_heads", [(1 << 60, 16), (1 << 62, 4), ((1 << 63) - 1, 2),
+                                       ((1 << 31) // 4, 4)])
+def test_more_rows_of_queries_than_32_bits_count(T, q_heads):
+    """T · q_heads is 2^64 (0 in 64 bits), or more than 2^31 - 1."""
+    refused(SHAPE, _lib.attend_workspace, cache(heads=2), attend_args(T=T, q_heads=q_heads))
