@@ -6,13 +6,17 @@ says what each computes and how the cache lies in memory).
 Streams: a call runs on `stream`, or on the current one of its tensors' device,
 after what that stream holds already: work on other streams that its tensors wait
 for is the caller's to order.  Tensors that it allocates (results that no `out` was
-given for, workspaces) belong to the stream it runs on.  Everything on the device
-is asynchronous, and may be captured into a graph.
+given for, workspaces) belong to the stream it runs on.  Tensors handed to a call with
+a torch stream may be dropped at once: their memory is not given out again before
+that stream has done with it.  Where a stream is named by its handle (an integer or an
+ExternalStream, which may end before they do) the caller holds them until it has.
+Everything on the device is asynchronous, and may be captured into a graph.
 """
 from __future__ import annotations
 
 import math
 from contextlib import nullcontext
+from functools import partial
 
 import numpy as np
 
@@ -30,23 +34,37 @@ _HERE = nullcontext()
 
 
 def _on(device, stream):
-    """(context to run a call in, its stream's handle)."""
+    """(context to run a call in, its stream's handle, and a function to call after it
+    with the tensors that it uses)."""
     if stream is None:
         index = device.index
         handle = torch._C._cuda_getCurrentRawStream(index)
         # (cheaper than torch.cuda.current_device(), which sees to the set-up that a
         # GPU tensor has had)
         if index == torch._C._cuda_getDevice():
-            return _HERE, handle
-        return torch.cuda.device(device), handle
+            return _HERE, handle, _of_current
+        return torch.cuda.device(device), handle, _of_current
+    lasting = not isinstance(stream, torch.cuda.ExternalStream)
     if not hasattr(stream, "cuda_stream"):
-        handle = int(stream)
+        handle, lasting = int(stream), False
         # (an ExternalStream of 0 would be a new stream)
         stream = (torch.cuda.ExternalStream(handle, device=device) if handle
                   else torch.cuda.default_stream(device))
     if stream.device != device:
         raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
-    return torch.cuda.stream(stream), stream.cuda_stream
+    return torch.cuda.stream(stream), stream.cuda_stream, (
+        partial(_of_stream, stream) if lasting else _of_current)
+
+
+def _of_current(*tensors):
+    pass
+
+
+def _of_stream(stream, *tensors):
+    """Keeps the memory of tensors from other streams' until `stream` has done with it."""
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
 
 
 def _new(like, dtype):
@@ -150,12 +168,13 @@ def rope(x, positions, rotary: Rotary, out=None, dtype=None, transpose=False, st
         raise ValueError(f"the rotary must be on {dev}, not on {rotary.device}")
     if out is not None and dtype is not None and out.dtype != dtype:
         raise ValueError("out has another dtype than asked for")
-    ctx, handle = _on(dev, stream)
+    ctx, handle, uses = _on(dev, stream)
     with ctx:
         if out is None:
             out = _new(x, dtype or x.dtype)
         _lib.rope(T, heads, dim, cx, pos, rotary._c, transpose, _rows("out", out, shape, dev),
                   handle)
+        uses(x, positions, rotary.freq, out)
     return out
 
 
@@ -190,6 +209,7 @@ class KVCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.pages, self.heads, self.page_size, self.dim = pages, heads, page, dim
         self.device, self.dtype = k.device, k.dtype
+        self._tensors = (k, v, k_scale, v_scale)
         self._c = _lib.KVCacheDesc(kind, heads, dim, page, pages, k.data_ptr(), v.data_ptr(),
                                    *((t.data_ptr() for t in scales) if scales else (None, None)))
         _lib.check_cache(self._c)
@@ -239,12 +259,14 @@ class KVCache:
                 raise ValueError("out has another dtype than asked for")
         elif out is not None or dtype is not None:
             raise ValueError("out and dtype are of the turned q")
-        ctx, handle = _on(dev, stream)
+        ctx, handle, uses = _on(dev, stream)
         with ctx:
             if q is not None and out is None:
                 out = _new(q, dtype or q.dtype)
             _lib.cache_write(self._c, T, ck, cv, at, pos, turn, q_heads, cq,
                              None if q is None else _rows("out", out, q_shape, dev), handle)
+            uses(*self._tensors, k, v, slots, positions, None if rotary is None else rotary.freq,
+                 q, out)
         return out
 
     def read(self, slots, dtype=None, out=None, stream=None):
@@ -253,7 +275,7 @@ class KVCache:
         T = slots.numel()
         at = _index("slots", slots, torch.int64, T, self.device)
         shape = (T, self.heads, self.dim)
-        ctx, handle = _on(self.device, stream)
+        ctx, handle, uses = _on(self.device, stream)
         with ctx:
             if out is None:
                 out = tuple(torch.empty(shape, dtype=dtype or torch.float16, device=self.device)
@@ -263,6 +285,7 @@ class KVCache:
             k, v = out
             ck, cv = _rows("k", k, shape, self.device), _rows("v", v, shape, self.device)
             _lib.cache_read(self._c, T, at, ck, cv, handle)
+            uses(*self._tensors, slots, k, v)
         return k, v
 
     def attend(self, q, page_table, kv_len, q_start=None, max_new=None, causal=True, window=0,
@@ -305,7 +328,7 @@ class KVCache:
         if out is not None and (out.dtype != q.dtype or out.shape != q.shape
                                 or out.stride(2) != 1 or out.device != dev):
             raise ValueError("out must have q's type, shape and device and unit stride along a head")
-        ctx, handle = _on(dev, stream)
+        ctx, handle, uses = _on(dev, stream)
         with ctx:
             if out is None:
                 out = _new(q, q.dtype)
@@ -321,4 +344,5 @@ class KVCache:
                 room = torch.empty(size, dtype=torch.uint8, device=dev)
                 args.workspace, args.workspace_bytes = room.data_ptr(), size
             _lib.attend(self._c, args, handle)
+            uses(*self._tensors, q, page_table, kv_len, q_start, out)
         return (out, lse) if with_lse else out
