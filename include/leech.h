@@ -590,7 +590,9 @@ int leech_cache_read(const leech_kv_cache* cache, int64_t T, const int64_t* d_sl
  * to [0, T], L_b to [0, table_pages · page_size], and a page that is not in
  * [0, pages) makes the rows that see it NaN.  A number that is not finite, in a
  * key, value or scale, reaches only the rows that see its token, and makes
- * them not finite; what pages hold from L_b on never matters.  The result does
+ * them not finite, unless it is an infinity of a key or a key's scale that makes
+ * a score −inf: that weighs 0, and a row of no other scores is as one that sees
+ * nothing.  What pages hold from L_b on never matters.  The result does
  * not depend on the other sequences' contents, but on how the work is split,
  * which goes by all lengths. */
 typedef struct {

@@ -182,3 +182,54 @@ def test_scales_at_the_end_of_their_range(dev, new, q_type, cache_type, size, sc
     bound = 2 * U[q_type] * np.abs(v64).mean(0) + 2.0 ** -20
     assert (np.abs(f64(out)[:, 0] - v64.mean(0)) <= bound).all()
     assert (np.abs(f64(lse) - math.log(n)) <= 2.0 ** -18).all()
+
+
+@pytest.mark.parametrize("kind,part", [("f16", "key"), ("bf16", "key"), ("int8", "scale"),
+                                       ("e4m3", "scale")])
+@pytest.mark.parametrize("scale", [0.125, -0.125])
+@pytest.mark.parametrize("new", [2, 60])
+def test_infinite_scores(dev, new, scale, kind, part):
+    """An infinite key, or key scale, on the token that only the last row sees: a score
+    of +inf makes that row NaN, one of -inf leaves it as it is without the token.  A row
+    that sees only such a token is as one that sees nothing."""
+    n, dim = 100, 64
+    rng = np.random.default_rng(7)
+    q_type = "bf16" if kind == "bf16" else "f16"
+    k, v = (numbers(rng, (n, 1, dim), "f32") for _ in range(2))
+    q = numbers(rng, (new, 1, dim), q_type)
+    k[-1] = 2 * q[-1:].float()                                  # a positive product
+    q = q.to(dev)
+    slots, table = torch.arange(n).to(dev), torch.arange(7, dtype=torch.int32, device=dev).view(1, -1)
+    starts = torch.tensor([0, new], dtype=torch.int32, device=dev)
+    lens = torch.tensor([n], dtype=torch.int32, device=dev)
+    cache = P.KVCache.empty(7, 16, 1, dim, TYPES[kind], dev)
+    cache.write(k.to(dev), v.to(dev), slots)
+    clean, clean_lse = cache.attend(q, table, lens, starts, scale=scale, with_lse=True)
+    k64, v64 = (f64(t) for t in cache.read(slots, dtype=torch.float32))
+    want, want_lse, w = O.attend64(f64(q[-1:]), k64[:-1], v64[:-1], 1, n - 1, scale=scale)
+    place = (6, 0, (n - 1) % 16)
+    for sign in (1.0, -1.0):
+        if part == "key":
+            d = int(q[-1, 0].abs().argmax())
+            saved = cache.k[place][d].clone()
+            cache.k[place][d] = math.copysign(math.inf, sign * float(q[-1, 0, d]))
+        else:
+            saved = cache.k_scale[place].clone()
+            cache.k_scale[place] = sign * math.inf
+        out, lse = cache.attend(q, table, lens, starts, scale=scale, with_lse=True)
+        assert (out[:-1] == clean[:-1]).all() and (lse[:-1] == clean_lse[:-1]).all()
+        one, one_lse = cache.attend(q, table, lens, starts, scale=scale, window=1, with_lse=True)
+        if sign * scale > 0:
+            assert torch.isnan(out[-1]).all() and torch.isnan(lse[-1]).all()
+            assert torch.isnan(one[-1]).all() and torch.isnan(one_lse[-1]).all()
+        else:
+            av = w[0] @ np.abs(v64[:-1, 0])
+            es = (dim + 8) * 2.0 ** -24 * 0.125 * (np.abs(f64(q[-1, 0])) @ np.abs(k64[:-1, 0]).T).max() + 2.0 ** -21
+            bound = (U[q_type] + 2 * es) * av + U[q_type] * np.abs(want[0]) + 2.0 ** -25
+            assert (np.abs(f64(out[-1]) - want[0]) <= bound).all()
+            assert (np.abs(f64(lse[-1]) - want_lse[0]) <= es + 2.0 ** -21 * (1 + np.abs(want_lse[0]))).all()
+            assert (one[-1] == 0).all() and (one_lse[-1] == -math.inf).all()
+        if part == "key":
+            cache.k[place][d] = saved
+        else:
+            cache.k_scale[place] = saved
