@@ -514,8 +514,10 @@ typedef struct {
   int32_t interleaved;     /* 0 or 1                                                 */
 } leech_rotary;
 
-/* out = x turned by its tokens' positions (int64 [T], device, any sign; an angle
- * is off by at most 2^-51 of itself up to position 2^53).  transpose = 1 turns by the opposite angles, times the same
+/* out = x turned by its tokens' positions (int64 [T], device, any sign).  Up to
+ * position 2^53 an angle is off by at most 2^-51 of itself, for the f64 product, and
+ * 2^-24 of what the reduction to half a turn either way leaves of it, for the f32
+ * that sine and cosine take.  transpose = 1 turns by the opposite angles, times the same
  * magnitude: the gradient's pass, and the inverse where the magnitude is 1.  dim is a
  * multiple of 8 up to 256; out's rows must not overlap one another; out may be
  * x itself (same pointer, type and strides).  T = 0 does nothing.  Asynchronous on `stream`.
@@ -561,8 +563,8 @@ int leech_cache_write(const leech_kv_cache* cache, int64_t T, const leech_rows* 
                       const leech_rotary* rotary, int32_t q_heads, const leech_rows* q,
                       const leech_rows* q_out, void* stream);
 
-/* Read T slots back as rows of f32, f16 or bf16, both of one type (code · scale,
- * rounded once); a slot below 0 or past the cache reads as zeros.  Slots may repeat.
+/* Read T slots back as rows of f32, f16 or bf16, both of one type (of codes the f32
+ * product code · scale, rounded to the type); a slot below 0 or past the cache reads as zeros.  Slots may repeat.
  * Asynchronous on `stream`. */
 int leech_cache_read(const leech_kv_cache* cache, int64_t T, const int64_t* d_slots,
                      const leech_rows* k_out, const leech_rows* v_out, void* stream);

@@ -214,9 +214,15 @@ __device__ __forceinline__ uint32_t codes4(int type, const float v[4], float sca
   for (int t = 0; t < 4; ++t) w |= code_of(type, v[t], scale) << (8 * t);
   return w;
 }
-__device__ __forceinline__ float code_value(int type, uint32_t code) {
-  if (type == LEECH_INT8) return (float)(int8_t)code;
-  return __builtin_amdgcn_cvt_f32_fp8((int)code, 0);
+// The number that a code stands for: an f32 product, whatever it is rounded to next.
+// (It is made opaque: the compiler otherwise makes one instruction, and one rounding, of
+// some of the products and their f16 results, and a key differs from a value of the same
+// code and scale.)
+__device__ __forceinline__ float code_value(int type, uint32_t code, float scale) {
+  float v = scale * (type == LEECH_INT8 ? (float)(int8_t)code
+                                        : __builtin_amdgcn_cvt_f32_fp8((int)code, 0));
+  asm("" : "+v"(v));
+  return v;
 }
 
 // ------------------------------------------------------------------- writing
@@ -474,7 +480,7 @@ __device__ __forceinline__ void values8(int type, const kv_u32x4& w, float scale
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     if (type_bytes(type) == 1) {
-      v[e] = code_value(type, w[e >> 2] >> (8 * (e & 3)) & 0xFFu) * scale;
+      v[e] = code_value(type, w[e >> 2] >> (8 * (e & 3)) & 0xFFu, scale);
     } else {
       const uint32_t h = w[e >> 1] >> (16 * (e & 1)) & 0xFFFFu;
       v[e] = type == LEECH_F16 ? half_value(h) : bf16_value(h);
@@ -569,7 +575,7 @@ __device__ __forceinline__ void read_values(const ReadArgs& a, int64_t group) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           if (size == 1) {
-            v[e] = code_value(a.c.type, w[e][j >> 2] >> (8 * (j & 3)) & 0xFFu) * scale[j];
+            v[e] = code_value(a.c.type, w[e][j >> 2] >> (8 * (j & 3)) & 0xFFu, scale[j]);
           } else {
             const uint32_t x = w[e][(j >> 1) & 1] >> (16 * (j & 1)) & 0xFFFFu;
             v[e] = a.c.type == LEECH_F16 ? half_value(x) : bf16_value(x);

@@ -233,3 +233,23 @@ def test_infinite_scores(dev, new, scale, kind, part):
             cache.k[place][d] = saved
         else:
             cache.k_scale[place] = saved
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+def test_codes_read_as_the_rounded_f32_product(dev, kind):
+    """To the bit, for every code, in each type."""
+    rng = np.random.default_rng(8)
+    n, heads, dim = 64, 2, 256
+    cache = P.KVCache.empty(4, 16, heads, dim, TYPES[kind], dev)
+    codes = torch.arange(256, dtype=torch.int16).to(torch.uint8).view(TYPES[kind])
+    cache.k.copy_(codes.to(dev).expand_as(cache.k))
+    cache.v.copy_(codes.to(dev)[:, None].expand_as(cache.v))
+    for t in (cache.k_scale, cache.v_scale):
+        t.copy_(torch.from_numpy(np.exp2(rng.uniform(-12, 2, t.shape)).astype(np.float32)))
+    slots = torch.from_numpy(rng.permutation(n)).to(dev)
+    for dst in ("f32", "f16", "bf16"):
+        for got, scale in zip(cache.read(slots, dtype=TYPES[dst]), (cache.k_scale, cache.v_scale)):
+            s = scale.transpose(1, 2).reshape(n, heads)[slots]          # [pages, heads, page]
+            want = (codes.float().to(dev) * s[..., None]).to(TYPES[dst])
+            assert torch.equal(got.nan_to_num(7.0), want.nan_to_num(7.0))
+            assert torch.equal(got.isnan(), want.isnan())
