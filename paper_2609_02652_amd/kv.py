@@ -16,7 +16,6 @@ from __future__ import annotations
 
 import math
 from contextlib import nullcontext
-from functools import partial
 
 import numpy as np
 
@@ -34,16 +33,16 @@ _HERE = nullcontext()
 
 
 def _on(device, stream):
-    """(context to run a call in, its stream's handle, and a function to call after it
-    with the tensors that it uses)."""
+    """(context to run a call in, its stream's handle, and the stream if the call's
+    tensors have to be kept for it)."""
     if stream is None:
         index = device.index
         handle = torch._C._cuda_getCurrentRawStream(index)
         # (cheaper than torch.cuda.current_device(), which sees to the set-up that a
         # GPU tensor has had)
         if index == torch._C._cuda_getDevice():
-            return _HERE, handle, _of_current
-        return torch.cuda.device(device), handle, _of_current
+            return _HERE, handle, None
+        return torch.cuda.device(device), handle, None
     lasting = not isinstance(stream, torch.cuda.ExternalStream)
     if not hasattr(stream, "cuda_stream"):
         handle, lasting = int(stream), False
@@ -52,16 +51,11 @@ def _on(device, stream):
                   else torch.cuda.default_stream(device))
     if stream.device != device:
         raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
-    return torch.cuda.stream(stream), stream.cuda_stream, (
-        partial(_of_stream, stream) if lasting else _of_current)
+    return torch.cuda.stream(stream), stream.cuda_stream, stream if lasting else None
 
 
-def _of_current(*tensors):
-    pass
-
-
-def _of_stream(stream, *tensors):
-    """Keeps the memory of tensors from other streams' until `stream` has done with it."""
+def _keep(stream, *tensors):
+    """Keeps the memory of tensors from other uses until `stream` has done with it."""
     for t in tensors:
         if t is not None:
             t.record_stream(stream)
@@ -168,13 +162,14 @@ def rope(x, positions, rotary: Rotary, out=None, dtype=None, transpose=False, st
         raise ValueError(f"the rotary must be on {dev}, not on {rotary.device}")
     if out is not None and dtype is not None and out.dtype != dtype:
         raise ValueError("out has another dtype than asked for")
-    ctx, handle, uses = _on(dev, stream)
+    ctx, handle, side = _on(dev, stream)
     with ctx:
         if out is None:
             out = _new(x, dtype or x.dtype)
         _lib.rope(T, heads, dim, cx, pos, rotary._c, transpose, _rows("out", out, shape, dev),
                   handle)
-        uses(x, positions, rotary.freq, out)
+        if side:
+            _keep(side, x, positions, rotary.freq, out)
     return out
 
 
@@ -259,14 +254,14 @@ class KVCache:
                 raise ValueError("out has another dtype than asked for")
         elif out is not None or dtype is not None:
             raise ValueError("out and dtype are of the turned q")
-        ctx, handle, uses = _on(dev, stream)
+        ctx, handle, side = _on(dev, stream)
         with ctx:
             if q is not None and out is None:
                 out = _new(q, dtype or q.dtype)
             _lib.cache_write(self._c, T, ck, cv, at, pos, turn, q_heads, cq,
                              None if q is None else _rows("out", out, q_shape, dev), handle)
-            uses(*self._tensors, k, v, slots, positions, None if rotary is None else rotary.freq,
-                 q, out)
+            if side:
+                _keep(side, *self._tensors, k, v, slots, positions, rotary and rotary.freq, q, out)
         return out
 
     def read(self, slots, dtype=None, out=None, stream=None):
@@ -275,7 +270,7 @@ class KVCache:
         T = slots.numel()
         at = _index("slots", slots, torch.int64, T, self.device)
         shape = (T, self.heads, self.dim)
-        ctx, handle, uses = _on(self.device, stream)
+        ctx, handle, side = _on(self.device, stream)
         with ctx:
             if out is None:
                 out = tuple(torch.empty(shape, dtype=dtype or torch.float16, device=self.device)
@@ -285,7 +280,8 @@ class KVCache:
             k, v = out
             ck, cv = _rows("k", k, shape, self.device), _rows("v", v, shape, self.device)
             _lib.cache_read(self._c, T, at, ck, cv, handle)
-            uses(*self._tensors, slots, k, v)
+            if side:
+                _keep(side, *self._tensors, slots, k, v)
         return k, v
 
     def attend(self, q, page_table, kv_len, q_start=None, max_new=None, causal=True, window=0,
@@ -328,7 +324,7 @@ class KVCache:
         if out is not None and (out.dtype != q.dtype or out.shape != q.shape
                                 or out.stride(2) != 1 or out.device != dev):
             raise ValueError("out must have q's type, shape and device and unit stride along a head")
-        ctx, handle, uses = _on(dev, stream)
+        ctx, handle, side = _on(dev, stream)
         with ctx:
             if out is None:
                 out = _new(q, q.dtype)
@@ -344,5 +340,6 @@ class KVCache:
                 room = torch.empty(size, dtype=torch.uint8, device=dev)
                 args.workspace, args.workspace_bytes = room.data_ptr(), size
             _lib.attend(self._c, args, handle)
-            uses(*self._tensors, q, page_table, kv_len, q_start, out)
+            if side:
+                _keep(side, *self._tensors, q, page_table, kv_len, q_start, out)
         return (out, lse) if with_lse else out
