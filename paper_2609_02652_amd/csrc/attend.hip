@@ -1200,6 +1200,12 @@ int cut(const leech_attend_args* g, const CacheShape& c, bool many, Cut* k) {
   k->whole_few = many ? 1024 >> k->log_step : 3 * k->waves;
   k->whole_many = many ? k->whole_few : (k->block_rows > 16 ? 4 : 8) * k->waves;
   k->split = keys > ((int64_t)k->whole_few << k->log_step) && least * c.heads < k->target;
+  // Few rows are a tile a sequence, however few they are.  Where those fill the card
+  // eight times over (4096 workgroups) they stay whole: every wave would number all of
+  // them (f16, 8 heads and as many of the queries, dim 128: 1000 sequences of 300 keys
+  // 820 us split, 311 whole, one of them of 30000 keys 850 and 371; 512 sequences 301
+  // and 165, 310 and 351; 256 sequences 122 and 84, 134 and 345: split).
+  if (!many && std::min<int64_t>(g->B, g->T) * c.heads >= 8 * k->target) k->split = 0;
   // (two more for the roundings of the plan's f32 total)
   k->tiles = T / k->block_rows + std::min<int64_t>(g->B, g->T);
   // Few rows are one tile a sequence: unsplit, nothing has to be looked for

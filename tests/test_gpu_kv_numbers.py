@@ -11,7 +11,7 @@ torch = pytest.importorskip("torch")
 
 import paper_2609_02652_amd as P  # noqa: E402
 from oracle import kv as O  # noqa: E402
-from test_gpu_kv import TYPES, U, f64, numbers, say  # noqa: E402
+from test_gpu_kv import Batch, TYPES, U, f64, numbers, say  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -253,3 +253,16 @@ def test_codes_read_as_the_rounded_f32_product(dev, kind):
             want = (codes.float().to(dev) * s[..., None]).to(TYPES[dst])
             assert torch.equal(got.nan_to_num(7.0), want.nan_to_num(7.0))
             assert torch.equal(got.isnan(), want.isnan())
+
+
+@pytest.mark.parametrize("cache_type", ["f16", "e4m3"])
+def test_more_single_tokens_than_the_card_takes_at_once(dev, cache_type):
+    """1100 sequences of 4 heads stay whole, however long the table; empty ones too."""
+    rng = np.random.default_rng(9)
+    lens = [(1, int(n)) for n in rng.integers(0, 40, 1100)]
+    lens[7], lens[1000] = (1, 2000), (1, 1)
+    b = Batch(dev, 33, lens, 4, 4, 32, 16, "f16", cache_type)
+    for starts in (None, b.q_start):
+        out, lse = b.attend(q_start=starts, max_new=None if starts is None else 1, with_lse=True)
+        torch.cuda.synchronize()
+        b.check(out, lse)
