@@ -520,7 +520,8 @@ typedef struct {
  * that sine and cosine take.  transpose = 1 turns by the opposite angles, times the same
  * magnitude: the gradient's pass, and the inverse where the magnitude is 1.  dim is a
  * multiple of 8 up to 256; out's rows must not overlap one another; out may be
- * x itself (same pointer, type and strides).  T = 0 does nothing.  Asynchronous on `stream`.
+ * x itself (same pointer, type and strides), else it shares no element with another
+ * array of the call (so too for the outputs of the calls below).  T = 0 does nothing.  Asynchronous on `stream`.
  * LEECH_E_ARG for a NULL or misaligned pointer, an unknown type, a magnitude
  * that is not positive and finite; LEECH_E_SHAPE for sizes outside the ranges
  * above or output rows that overlap. */
@@ -553,8 +554,9 @@ typedef struct {
 /* Write T tokens' keys and values into their slots (int64 [T], device), the
  * keys turned first where a rotary is given (NULL: as they are; d_positions as
  * leech_rope, else unused).  A slot below 0 or past the cache is skipped (a
- * padded batch's rows); slots must differ, or which token's numbers a shared
- * slot holds is open.  q_heads > 0 (with a rotary) also turns q into q_out in
+ * padded batch's rows).  Slots that are not skipped must differ: a shared one may
+ * end up with some numbers of each of its tokens, codes of one and the scale of
+ * another among them.  q_heads > 0 (with a rotary) also turns q into q_out in
  * the same launch, for every token; q_out may be q itself.  Asynchronous on `stream`.
  * LEECH_E_ARG and LEECH_E_SHAPE as leech_rope, and for a cache that is not as
  * described; k, v and q must be of one type (LEECH_E_ARG). */
@@ -615,7 +617,8 @@ typedef struct {
   const int32_t* page_table;  /* [B] rows of table_pages, table_stride apart         */
   int64_t table_stride;
   int32_t table_pages;
-  int32_t max_new;         /* at least every n_b (rows past it are left as they are) */
+  int32_t max_new;         /* at least every n_b (rows past it are left as they      */
+                           /* are); the larger, the more launches and workspace      */
   int32_t causal;          /* 0 or 1                                                 */
   int32_t window;          /* 0: none                                                */
   float scale;             /* finite                                                 */

@@ -227,7 +227,7 @@ class KVCache:
               dtype=None, stream=None):
         """Keep the tokens k, v [T, heads, dim] (f32, f16 or bf16, any token and
         head strides) in slots int64 [T] (page · page_size + place; out of range:
-        not kept), k turned by positions int64 [T] first if a rotary is given.
+        not kept; otherwise no two alike), k turned by positions int64 [T] first if a rotary is given.
         With q [T, q_heads, dim], the same launch turns q into `out` (or a new
         tensor of `dtype`, q's if None) and returns it."""
         T, dev = k.shape[0], self.device
@@ -291,7 +291,8 @@ class KVCache:
         rows q_start[b] to q_start[b + 1] (int32 [B + 1]; None: one each, T = B);
         page_table int32 [B, table_pages]; kv_len int32 [B] counts the cached
         tokens, the new ones among them.  max_new: at least every sequence's new
-        tokens (None: T).  window > 0: a query sees the last `window` keys up to its
+        tokens (None: 1 without q_start, else T; the kernels, launches and workspace go by
+        it, so a batch of few new tokens each is quicker with it given).  window > 0: a query sees the last `window` keys up to its
         own.  scale: None for dim^-1/2.  `out` may be q.  Returns out [T, q_heads, dim] of q's type
         (rows of no sequence are not written), and lse f32 [T, q_heads] with
         with_lse."""
