@@ -14,8 +14,12 @@
 //
 // One pass.  A query keeps a base (of two's powers), the sum l of its weights
 // 2^(s − base) and O; the base follows the largest score seen, but only once that
-// is far enough above it, and l and O are scaled to it.  Weights are rounded to the
-// products' type for the second product.  In f16 the base stays 2^11 to 2^15 under the
+// is far enough above it, and l and O are scaled to it.  The second product takes
+// weights rounded to its type: with a second number for what that leaves off, out is as
+// good as f32 weights make it (64 sequences of up to 8000 bf16 keys: off by 0.17%, 0.23%
+// with one), but a 4096-token prompt takes 235 us (178), 4 x 999 tokens over int8 1052
+// (819), 16 x 5 28.7 (27.3), and rows would depend on the kernel that takes them if only
+// stream_kernel, which mostly waits for memory, did it.  In f16 the base stays 2^11 to 2^15 under the
 // largest score: the large weights fill f16's range from the top, so that the many
 // small ones of a long context are numbers too.  Rows are (new token, query head of
 // the group) of one sequence and cache head, so a group's heads share every key read.
