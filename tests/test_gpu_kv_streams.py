@@ -96,3 +96,30 @@ def test_streams_named_by_their_handle(dev, how):
     got = run("attend", cache, turn, i, stream)
     torch.cuda.synchronize()
     assert (got == want).all()
+
+
+def test_a_call_captured_on_a_given_stream(dev):
+    """The capture's own stream is named, its tensors are from outside; replays beside
+    eager work, and calls after their memory is given back."""
+    turn, i = P.Rotary.of(DIM, device=dev), inputs(dev)
+    cache = P.KVCache.empty(3, PAGE, HEADS, DIM, torch.int8, dev)
+    run("write", cache, turn, i)
+    want = run("attend", cache, turn, i)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        stream = torch.cuda.current_stream()
+        run("write", cache, turn, i, stream)
+        got = run("attend", cache, turn, i, stream)
+    for turn_no in range(3):
+        i["v"].mul_(-1)                                 # v is linear in the output
+        run("read", cache, turn, i)
+        got.fill_(5)
+        g.replay()
+        torch.cuda.synchronize()
+        assert (got == (want if turn_no % 2 else -want)).all()
+    del i, cache, got, g
+    i, cache = inputs(dev), P.KVCache.empty(3, PAGE, HEADS, DIM, torch.int8, dev)
+    again = run("attend", cache, turn, i)
+    torch.cuda.synchronize()
+    assert (again == 0).all()                           # an empty cache's values
